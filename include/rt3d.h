@@ -377,6 +377,158 @@ rt3d_status rt3d_group_reweight(const rt3d_group_desc *desc, const void *w, cons
                                 float *grad, void *w_prox,
                                 void *workspace, uint64_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Token operators
+ *
+ * A conv trunk leaves a grid of feature vectors per clip, channels last: its
+ * voxels are tokens.  Token blocks on top of it normalise every vector, project
+ * it (1x1x1 convs), rotate queries and keys by the token's place in the grid and
+ * attend.  The calls below are those operators and their backward passes.
+ * They follow the conventions at the top, except that they need finite values
+ * only where they say so, and that pointers of layer norm and of the rotation
+ * need only the alignment of an element (16-byte aligned pointers and pitches
+ * of whole 16 bytes are faster).  Sums, statistics and softmax are float32 with a
+ * fixed order: repeated calls give identical results.  Calls may be captured.
+ * ------------------------------------------------------------------------ */
+
+/* Layout of a batch of token rows: elements between neighbouring tokens of a
+ * clip and between clips.  0 = tight. */
+typedef struct {
+    int64_t pitch, batch;
+} rt3d_rows;
+
+/* Layer norm over the c channels of every row (voxel, token, or a head's vector):
+ *   mean = sum x / c,  rstd = 1 / sqrt(sum (x - mean)^2 / c + eps),
+ *   y = (x - mean) * rstd * gamma + beta. */
+typedef struct {
+    int64_t rows;
+    int32_t c;                /* 1 .. 2^20 */
+    int32_t dtype;            /* rt3d_dtype of x, y, dy, dx */
+    float eps;                /* > 0 */
+    int64_t x_pitch, y_pitch; /* elements per row of x and dx, of y and dy; 0 = c */
+} rt3d_norm_desc;
+
+/* gamma, beta: float32 [c] or NULL (ones, zeros).  mean, rstd: float32 [rows],
+ * what the backward pass needs, or NULL.  y may be x where the pitches are equal.
+ * Elements of y between c and its pitch are not written.  rows = 0: nothing is
+ * read or written. */
+rt3d_status rt3d_layernorm_fwd(const rt3d_norm_desc *desc, const void *x, const float *gamma,
+                               const float *beta, void *y, float *mean, float *rstd, void *stream);
+
+/* Device workspace (bytes, 4-byte aligned) of a backward call that is asked for
+ * dgamma or dbeta: partial sums over the rows.  No initial contents are needed;
+ * calls that share a workspace must not overlap in time.  Host only. */
+rt3d_status rt3d_layernorm_bwd_workspace_size(const rt3d_norm_desc *desc, uint64_t *bytes);
+
+/* With h = (x - mean) * rstd and g = dy * gamma:
+ *   dx     = rstd * (g - mean_c(g) - h * mean_c(g * h))      (desc->dtype)
+ *   dgamma = sum over rows of dy * h,  dbeta = sum over rows of dy   (float32 [c])
+ * dx, dgamma and dbeta may each be NULL (not computed); they must not overlap the
+ * inputs or each other.  They are written, not added to; rows = 0 gives zero
+ * dgamma and dbeta. */
+rt3d_status rt3d_layernorm_bwd(const rt3d_norm_desc *desc, const void *x, const void *dy,
+                               const float *gamma, const float *mean, const float *rstd,
+                               void *dx, float *dgamma, float *dbeta,
+                               void *workspace, uint64_t workspace_bytes, void *stream);
+
+enum {
+    RT3D_ROPE_HALVES = 1u,    /* pair i of a section of s channels is (i, i + s/2);
+                                 otherwise (2i, 2i + 1) */
+    RT3D_ROPE_INVERSE = 2u    /* turn the other way: the transpose, which is the
+                                 backward pass and undoes the rotation */
+};
+
+/* Rotary positions along three axes.  The first dt channels of a vector turn
+ * with the token's time, the next dh with its row, the next dw with its column;
+ * the rest is copied.  Pair i of a section of s channels turns by
+ *   angle = position * base^(-2 i / s):
+ *   (a, b) -> (a cos - b sin, a sin + b cos).
+ * Angles are formed in 64 bits (streams run to far positions). */
+typedef struct {
+    int32_t n, t, h, w;       /* clips and their token grid; tokens are t-major */
+    int32_t vecs, d;          /* vectors of a token (heads of queries and keys side by
+                                 side) and their channels; d even */
+    int32_t dt, dh, dw;       /* channels of the sections, even, at most d together */
+    int32_t t0;               /* time of the first frame, for grid positions */
+    float base;               /* > 0 */
+    int32_t dtype;            /* rt3d_dtype of x and y */
+    uint32_t flags;           /* RT3D_ROPE_HALVES | RT3D_ROPE_INVERSE */
+    rt3d_rows x, y;           /* rows of vecs * d elements */
+} rt3d_rope_desc;
+
+/* pos: int32 [n][t*h*w][3] device array of (time, row, column) per token, any
+ * values, or NULL: the token's place in the grid, time from t0 on.  y may be x
+ * with one layout (in place); otherwise they must not overlap.  Pairs of
+ * neighbours need even pitches and batch strides and pointers aligned to a pair
+ * (RT3D_ERR_UNSUPPORTED). */
+rt3d_status rt3d_rope3d(const rt3d_rope_desc *desc, const void *x, const int32_t *pos, void *y,
+                        void *stream);
+
+/* Differential attention.  Each of hq query heads has two query vectors of d
+ * channels, each of hk key heads two key vectors and one value vector of 2 d
+ * channels; query head j uses key head j / (hq / hk).  Over the visible keys
+ *   P_m = softmax(scale * q_m k_m^T)  for m = 1, 2,   o = (P_1 - lambda_j P_2) v.
+ * Visible are the clip's keys (the first k_len of lk); with frame > 0 also only
+ * those of the query's own frame and of earlier ones, where a frame is `frame`
+ * tokens (1: ordinary causal attention) and the queries end where the keys end:
+ * query i of q_len stands at key position k_len - q_len + i.  A query that sees
+ * no key gives zeros. */
+typedef struct {
+    int32_t n, lq, lk;        /* clips, queries and keys of a (padded) clip */
+    int32_t hq, hk;           /* query and key heads, hq a multiple of hk */
+    int32_t d;                /* channels of a query or key vector: a multiple of 8 up to 128 */
+    int32_t dtype;            /* rt3d_dtype of q, k, v, o and their gradients */
+    int32_t frame;            /* tokens of a frame of the causal mask, 0 = no mask */
+    float scale;              /* 0 = 1 / sqrt(d) */
+    rt3d_rows q, o;           /* rows of hq * 2 * d elements: [hq][2][d], [hq][2 d] */
+    rt3d_rows k, v;           /* rows of hk * 2 * d elements: [hk][2][d], [hk][2 d] */
+    rt3d_rows d_o, dq, dk, dv; /* the same for the gradients (backward only) */
+} rt3d_diffattn_desc;
+
+/* Device workspace (bytes, 16-byte aligned) with which a forward call of few
+ * query rows runs at full parallelism: it splits the keys over workgroups and a
+ * second kernel joins them in their order.  A call given less (or none) uses
+ * fewer splits; it never fails for lack of workspace.  0 for calls of many rows.
+ * Depends on the padded lengths only.  Host only. */
+rt3d_status rt3d_diffattn_fwd_workspace_size(const rt3d_diffattn_desc *desc, uint64_t *bytes);
+
+/* lambda: float32 [hq].  q_len, k_len: int32 [n] device arrays, or NULL (lq, lk);
+ * values outside 0 .. lq (lk) count as the nearest bound.  Queries behind q_len
+ * and keys and values behind k_len are never read and may hold anything; o is
+ * zero in rows behind q_len.  Values of keys that only the frame mask hides must
+ * be finite.  o2 and lse are what the backward pass needs, or NULL: o2 the second
+ * map's output P_2 v, tight [n][lq][hq][2 d] in desc->dtype, lse float32
+ * [2][n][hq][lq], the base-2 logarithm of each map's softmax denominator.
+ * Pointers must be 16-byte aligned (lambda, lse and lengths 4), pitches and batch
+ * strides multiples of 16 bytes; a pitch is below 2^22 elements, lq * (hq / hk), lk
+ * and frame below 2^30.  n = 0 or lq = 0: nothing is read or written.  o and o2
+ * must not overlap the inputs or each other.  Scores, probabilities and sums are
+ * float32; probabilities (and in the backward pass the gradients of scores) are
+ * rounded to desc->dtype for the products, in fp16 to within 2^-25 below 2^-14:
+ * scale small output gradients up. */
+rt3d_status rt3d_diffattn_fwd(const rt3d_diffattn_desc *desc, const void *q, const void *k,
+                              const void *v, const float *lambda, const int32_t *q_len,
+                              const int32_t *k_len, void *o, void *o2, float *lse,
+                              void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Device workspace (bytes, 16-byte aligned) that a backward call needs.  Calls
+ * that share a workspace must not overlap in time.  Host only. */
+rt3d_status rt3d_diffattn_bwd_workspace_size(const rt3d_diffattn_desc *desc, uint64_t *bytes);
+
+/* Gradients of sum(o * d_o), from the inputs and what the forward call of the
+ * same desc, lambda and lengths left in o, o2 and lse: dq, dk, dv (desc->dtype;
+ * heads that share a key head add up before the one rounding) and dlambda
+ * (float32 [hq]).  Each may be NULL (not computed).  They are written, not added
+ * to; rows behind q_len and k_len are zero.  d_o is not read behind q_len.
+ * Outputs must not overlap the inputs or each other.  Needs workspace of
+ * rt3d_diffattn_bwd_workspace_size bytes (RT3D_ERR_BUFFER_TOO_SMALL otherwise). */
+rt3d_status rt3d_diffattn_bwd(const rt3d_diffattn_desc *desc, const void *q, const void *k,
+                              const void *v, const float *lambda, const int32_t *q_len,
+                              const int32_t *k_len, const void *o, const void *o2,
+                              const float *lse, const void *d_o, void *dq, void *dk, void *dv,
+                              float *dlambda, void *workspace, uint64_t workspace_bytes,
+                              void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,255 @@
+// Device code shared by the kernels of differential attention: MFMA fragments,
+// the staged tile and its swizzle, the mask.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <atomic>
+
+#include "rt3d_tokens.h"
+
+namespace rt3d {
+namespace attn {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(8 * sizeof(float)))) float f32x8;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+typedef __attribute__((address_space(3))) char lds_char;
+
+// A fragment: eight values along the reduction of one row (or column) of a 32x32
+// MFMA with 16 reduction steps.  Lane l holds row (column) l % 32, its half h =
+// l / 32 the steps 8 h .. 8 h + 7.  For 32-bit values the same eight go through
+// eight 32x32x2 products, value e of both halves in the e-th: only the order of
+// the sum differs.  Results: lane l holds column l % 32, register i the row
+// 8 (i / 4) + 4 h + i % 4.
+template <typename T>
+struct Mma;
+template <>
+struct Mma<__bf16> {
+  using Frag = bf16x8;
+  static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<_Float16> {
+  using Frag = f16x8;
+  static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<float> {
+  using Frag = f32x8;
+  static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+template <typename T>
+using Frag = typename Mma<T>::Frag;
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Waits for this wave's direct loads, then for the workgroup.
+__device__ __forceinline__ void tile_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Over the two halves of a row (lanes l and l + 32); both get the result.
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Eight consecutive values of a row in memory, 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ Frag<T> load_frag(const T *p) {
+  return *reinterpret_cast<const Frag<T> *>(p);
+}
+template <>
+__device__ __forceinline__ f32x8 load_frag<float>(const float *p) {
+  const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+  return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// A staged tile: ROWS rows (keys, or query rows) of 2 D values, unpadded (direct
+// loads fill LDS in the order of lanes), its 16-byte blocks permuted within
+// groups of 16 (8 where a row has only 8) by an XOR with a value of the row.  The
+// value makes both kinds of reads free of bank conflicts: 16 rows at one block
+// (operands along the row) and four rows at four neighbouring blocks (transposed
+// operands).
+template <typename T, int D, int ROWS, int THREADS>
+struct Tile {
+  static constexpr int kEs = sizeof(T);
+  static constexpr int kRowBytes = 2 * D * kEs;
+  static constexpr int kBlocks = kRowBytes / 16;          // 16-byte blocks of a row
+  static constexpr int kBytes = ROWS * kRowBytes;
+  static constexpr int kLoads = ROWS * kBlocks / THREADS; // direct loads of a thread
+  static_assert(ROWS * kBlocks % THREADS == 0, "a tile is whole loads of every thread");
+
+  static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (kBlocks == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
+    return ((row & 3) << 2) | ((row >> 2) & 3);
+  }
+
+  // Byte offsets of a thread's loads from the tile's first row in memory, or
+  // far out of any tile where the block is padding (d < D).  SPLIT: a row is two
+  // vectors of d padded to D each (queries, keys), else one of 2 d (values).
+  template <bool SPLIT>
+  static __device__ __forceinline__ void offsets(int d, int64_t pitch, unsigned (&off)[kLoads]) {
+    constexpr int kPer = 16 / kEs;  // values of a block
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = i * THREADS + static_cast<int>(threadIdx.x);
+      const int row = c / kBlocks, blk = (c % kBlocks) ^ swizzle(row);
+      int col = blk * kPer;
+      bool in;
+      if constexpr (SPLIT) {
+        const int m = col / D;
+        in = col - m * D < d;
+        col = m * d + col - m * D;
+      } else {
+        in = col < 2 * d;
+      }
+      off[i] = in ? static_cast<unsigned>((row * pitch + col) * kEs) : 0x80000000u;
+    }
+  }
+
+  // Starts the loads of `rows` (0..ROWS) rows from `first` on; the other rows
+  // of the tile become zeros.
+  static __device__ __forceinline__ void stage(const T *first, int rows, int d, int64_t pitch,
+                                               const unsigned (&off)[kLoads], lds_char *to) {
+    const int bytes = rows > 0 ? static_cast<int>(((rows - 1) * pitch + 2 * d) * kEs) : 0;
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(first), 0, bytes, 0x00020000);
+    const int wave = uniform(static_cast<int>(threadIdx.x) >> 6);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          r, (__attribute__((address_space(3))) void *)(to + (i * THREADS + wave * 64) * 16), 16,
+          static_cast<int>(off[i]), 0, 0, 0);
+  }
+
+  // Operand along the row: eight values from column `col` + 8 half of row `row`.
+  // col is a multiple of 16 and a constant; row0 + lane % 32.
+  static __device__ __forceinline__ Frag<T> along(const lds_char *t, int row0, int col) {
+    const int lane = threadIdx.x & 63, row = row0 + (lane & 31), f = swizzle(lane & 31);
+    const int half = lane >> 5;
+    if constexpr (kEs == 2) {
+      const int blk = col / 8, at = (blk & ~15) + (((blk & 15) | half) ^ f);
+      return *reinterpret_cast<const __attribute__((address_space(3))) Frag<T> *>(t + row * kRowBytes + at * 16);
+    } else {
+      const int blk = col / 4, at = (blk & ~15);
+      const auto *p = t + row * kRowBytes + at * 16;
+      const auto a = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(
+          p + ((((blk & 15) | (2 * half)) ^ f) * 16));
+      const auto b = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(
+          p + ((((blk & 15) | (2 * half) | 1) ^ f) * 16));
+      return Frag<T>{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
+  }
+
+  // Transposed operand: column `col` + lane % 32, and of the 16 rows from row0
+  // on those that a result's registers hold for the half: value e is row
+  // row0 + 8 (e / 4) + 4 half + e % 4.  row0 and col: multiples of 16 and 32.
+  static __device__ __forceinline__ Frag<T> across(const lds_char *t, int row0, int col) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    if constexpr (kEs == 2) {
+      // the transposing read: in 16 lanes, lane 4 r + c reads four values of row
+      // r, and receives those of its own column from four rows
+      const int r = (lane & 15) >> 2;
+      const int sub = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      union {
+        s16x4 half4[2];
+        Frag<T> all;
+      } u;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = row0 + 8 * j + 4 * half + r, blk = col / 8;
+        const int at = (blk & ~15) + (((blk & 15) | sub) ^ swizzle(row));
+        u.half4[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4 *)(t + row * kRowBytes + at * 16 + (lane & 1) * 8));
+      }
+      return u.all;
+    } else {
+      Frag<T> v;
+      const int c = col + (lane & 31);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int row = row0 + 8 * (e / 4) + 4 * half + e % 4, blk = c / 4;
+        const int at = (blk & ~15) + ((blk & 15) ^ swizzle(row));
+        v[e] = *reinterpret_cast<const __attribute__((address_space(3))) float *>(
+            t + row * kRowBytes + at * 16 + (c & 3) * 4);
+      }
+      return v;
+    }
+  }
+};
+
+// Eight result registers as an operand whose reduction runs over their rows (the
+// order that `across` reads the other operand in); rounded to the layer's type.
+template <typename T>
+__device__ __forceinline__ Frag<T> pack(const f32x16 &v, int from) {
+  Frag<T> f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = static_cast<T>(v[from + e]);
+  return f;
+}
+
+// Row of a result register.
+__device__ __forceinline__ int result_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
+
+// Keys visible to query i of a clip: the first `visible` ones.  The queries end
+// where the keys end; with frames, a query sees its own frame and those before.
+__device__ __forceinline__ int visible(int i, int q_len, int k_len, int frame) {
+  if (!frame) return k_len;
+  const int p = k_len - q_len + i;
+  if (p < 0) return 0;
+  const int64_t end = (static_cast<int64_t>(p / frame) + 1) * frame;
+  return end < k_len ? static_cast<int>(end) : k_len;
+}
+
+__device__ __forceinline__ int clip_length(const int32_t *len, int clip, int most) {
+  if (!len) return most;
+  const int v = len[clip];
+  return v < 0 ? 0 : v > most ? most : v;
+}
+
+// Workgroups of one clip and key head read the same keys (or queries): they are
+// dealt to one XCD (ids go round the eight), so that its L2 serves them.
+__device__ __forceinline__ int64_t logical_block(int64_t blocks) {
+  const int64_t per = (blocks + 7) / 8, id = blockIdx.x;
+  return (id % 8) * per + id / 8;
+}
+inline unsigned grid_of(int64_t blocks) { return static_cast<unsigned>((blocks + 7) / 8 * 8); }
+
+// Lets a kernel use more than the default 64 KB of LDS, once per device.
+template <auto K>
+int allow_lds(int bytes) {
+  if (bytes <= 65536) return hipSuccess;
+  constexpr int kMost = 64;
+  static std::atomic<bool> done[kMost];
+  int dev = 0;
+  const hipError_t got = hipGetDevice(&dev);
+  if (got != hipSuccess) return got;
+  const bool known = dev >= 0 && dev < kMost;
+  if (known && done[dev].load(std::memory_order_acquire)) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(K),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess && known) done[dev].store(true, std::memory_order_release);
+  return e;
+}
+
+}  // namespace attn
+}  // namespace rt3d

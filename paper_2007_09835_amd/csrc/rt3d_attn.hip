@@ -1,0 +1,333 @@
+// Differential attention on gfx950 (MI355X), forward.  Two softmax maps share
+// the values: with S_m = scale q_m k_m^T over the visible keys and P_m its softmax,
+//   o = P_1 v - lambda P_2 v,
+// v twice as wide as a query vector.  Queries of the heads that share a key head
+// are rows of one matrix, row r = query r / group of head r % group.
+
+#include "rt3d_attn.h"
+
+namespace rt3d {
+namespace {
+
+using namespace attn;
+
+// One wave holds 32 rows and walks the keys once with the running maximum and
+// sum of both maps.  S^T = K Q^T puts a row into a lane (and its other half), so
+// the softmax needs one exchange between halves, and the probabilities are the
+// second operand of O^T += V^T P^T where they stand: no trip through LDS.  Keys
+// and values are staged by direct loads, two tiles deep.  Up to d = 64 a wave
+// holds both maps, whose products share the value operands; beyond that their
+// 2 x 32 x 256 results would take every accumulator, so two waves hold one map
+// each of the same rows and meet at the end.
+// ROWS: groups of 32 rows of a workgroup.
+template <typename T, int D, int ROWS>
+struct Fwd {
+  static constexpr int kMaps = D > 64 ? 1 : 2;
+  static constexpr int kWaves = ROWS * 2 / kMaps;
+  static constexpr int kThreads = 64 * kWaves;
+  static constexpr int kKeys = ROWS == 1 || D > 64 ? 32 : 64;
+  static constexpr int kWidth = 2 * D;
+  using KV = Tile<T, D, kKeys, kThreads>;
+  static constexpr int kLds = 4 * KV::kBytes;
+  static constexpr int kMinWaves = sizeof(T) == 2 ? 2 : 1;
+  static_assert(kMaps == 2 || ROWS * 32 * kWidth * 4 <= kLds, "the second maps' results fit");
+};
+
+// log2 units by which a row's scores may pass its reference before everything is
+// scaled down to a new one: P <= 2^8 fits every type, and most tiles need no pass.
+constexpr float kSlack = 8.f;
+
+template <typename T, int D, int ROWS, bool SPLIT>
+__global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMinWaves)) void attn_fwd_kernel(
+    AttnArgs a) {
+  using F = Fwd<T, D, ROWS>;
+  using KV = typename F::KV;
+  constexpr int kKeys = F::kKeys, kSub = kKeys / 32, kTiles = F::kWidth / 32, kMaps = F::kMaps;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  lds_char *lds = (lds_char *)smem;
+
+  int64_t id = logical_block(a.blocks);
+  if (id >= a.blocks) return;
+  const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
+  if (SPLIT) id /= a.splits;
+  const int tile = a.tiles - 1 - static_cast<int>(id % a.tiles);  // rows with most keys first
+  id /= a.tiles;
+  const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
+
+  const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);
+  const int rows = a.lq * a.group, used = q_len * a.group;
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(static_cast<int>(threadIdx.x) >> 6);
+  const int map0 = kMaps == 1 ? wave & 1 : 0;  // first map of this wave
+  const int first = (tile * ROWS + wave * kMaps / 2) * 32, row = first + (lane & 31);
+  const int query = row / a.group, head = kvh * a.group + (row - query * a.group);
+  const bool in = row < used;
+  const int limit = in ? visible(query, q_len, k_len, a.frame) : 0x7fffffff;
+
+  // keys of the workgroup and of this wave (rows see at least as many as those before)
+  const int last_block = min(used, (tile + 1) * ROWS * 32) - 1, last_wave = min(used, first + 32) - 1;
+  int begin = 0, end = last_block < tile * ROWS * 32 ? 0 : visible(last_block / a.group, q_len, k_len, a.frame);
+  const int wave_end = last_wave < first ? 0 : visible(last_wave / a.group, q_len, k_len, a.frame);
+  const int whole = last_wave < first ? 0 : visible(first / a.group, q_len, k_len, a.frame);
+  if (SPLIT) {
+    begin = split * a.span;
+    end = min(end, begin + a.span);
+  }
+
+  f32x16 acc[kMaps][kTiles] = {};
+  float top[kMaps], sum[kMaps];
+#pragma unroll
+  for (int m = 0; m < kMaps; ++m) top[m] = -INFINITY, sum[m] = 0.f;
+
+  if (begin < end) {
+    Frag<T> q[kMaps][D / 16];
+    {
+      const T *p = static_cast<const T *>(a.q) + clip * a.q_batch + query * a.q_pitch +
+                   (static_cast<int64_t>(head) * 2 + map0) * a.d;
+#pragma unroll
+      for (int m = 0; m < kMaps; ++m)
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+          const int col = s * 16 + 8 * half;
+          q[m][s] = in && col < a.d ? load_frag(p + m * a.d + col) : Frag<T>{};
+        }
+    }
+    unsigned k_off[KV::kLoads], v_off[KV::kLoads];
+    KV::template offsets<true>(a.d, a.k_pitch, k_off);
+    KV::template offsets<false>(a.d, a.v_pitch, v_off);
+    const T *k = static_cast<const T *>(a.k) + clip * a.k_batch + static_cast<int64_t>(kvh) * 2 * a.d;
+    const T *v = static_cast<const T *>(a.v) + clip * a.v_batch + static_cast<int64_t>(kvh) * 2 * a.d;
+    auto stage = [&](int key, int buf) {
+      const int n = min(kKeys, k_len - key);
+      KV::stage(k + key * a.k_pitch, n, a.d, a.k_pitch, k_off, lds + buf * 2 * KV::kBytes);
+      KV::stage(v + key * a.v_pitch, n, a.d, a.v_pitch, v_off, lds + (buf * 2 + 1) * KV::kBytes);
+    };
+    stage(begin, 0);
+    int buf = 0;
+    for (int key = begin; key < end; key += kKeys, buf ^= 1) {
+      tile_barrier();  // this tile has landed, and the other buffer is read
+      if (key + kKeys < end) stage(key + kKeys, buf ^ 1);
+      if (key >= wave_end) continue;
+      const lds_char *kt = lds + buf * 2 * KV::kBytes, *vt = kt + KV::kBytes;
+      const bool masked = key + kKeys > whole;
+      Frag<T> p[kMaps][2 * kSub];
+#pragma unroll
+      for (int m = 0; m < kMaps; ++m) {
+        f32x16 s[kSub] = {};
+#pragma unroll
+        for (int j = 0; j < kSub; ++j)
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i)
+            s[j] = Mma<T>::run(KV::along(kt + map0 * D * KV::kEs, j * 32, m * D + i * 16), q[m][i], s[j]);
+        if (masked) {
+#pragma unroll
+          for (int j = 0; j < kSub; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (key + j * 32 + result_row(i, half) >= limit) s[j][i] = -INFINITY;
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int j = 0; j < kSub; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) most = fmaxf(most, s[j][i]);
+        most = half_max(most) * a.scale2;
+        if (__any(most > top[m] + kSlack)) {
+          const float now = fmaxf(top[m], most);
+          const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
+          top[m] = now;
+          sum[m] *= by;
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[m][t][i] *= by;
+        }
+        const float ref = top[m] == -INFINITY ? 0.f : -top[m];
+#pragma unroll
+        for (int j = 0; j < kSub; ++j) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[j][i] = __builtin_amdgcn_exp2f(fmaf(s[j][i], a.scale2, ref));
+            sum[m] += s[j][i];
+          }
+          // Rounded to the layer's type for the product with v (half a step of
+          // each probability); their sum keeps 32 bits.
+          p[m][2 * j] = pack<T>(s[j], 0);
+          p[m][2 * j + 1] = pack<T>(s[j], 8);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2 * kSub; ++s)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          const Frag<T> f = KV::across(vt, s * 16, t * 32);
+#pragma unroll
+          for (int m = 0; m < kMaps; ++m) acc[m][t] = Mma<T>::run(f, p[m][s], acc[m][t]);
+        }
+    }
+  }
+
+#pragma unroll
+  for (int m = 0; m < kMaps; ++m) sum[m] = half_sum(sum[m]);
+  if (SPLIT) {
+    if (!in) return;
+    const int64_t r = (static_cast<int64_t>(clip) * a.hk + kvh) * rows + row;
+    const int64_t total = static_cast<int64_t>(a.n) * a.hk * rows;
+    float *st = a.part + (split * total + r) * 4 + 2 * map0;
+    float *out = a.part + a.splits * total * 4 + (split * total + r) * 4 * a.d + 2 * map0 * a.d;
+#pragma unroll
+    for (int m = 0; m < kMaps; ++m) {
+      if (half == 0) {
+        st[2 * m] = top[m];
+        st[2 * m + 1] = sum[m];
+      }
+      if (sum[m] == 0.f) continue;  // no key here: nothing is read back
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int col = t * 32 + 8 * g + 4 * half;
+          if (col < 2 * a.d)
+            *reinterpret_cast<f32x4 *>(out + m * 2 * a.d + col) =
+                f32x4{acc[m][t][4 * g], acc[m][t][4 * g + 1], acc[m][t][4 * g + 2], acc[m][t][4 * g + 3]};
+        }
+    }
+    return;
+  }
+
+  // A row that sees no key, and rows behind the clip's end: zeros, and a
+  // logarithm of +inf, which makes every probability of the backward pass zero.
+  const bool any = in && sum[0] > 0.f;
+#pragma unroll
+  for (int m = 0; m < kMaps; ++m) {
+    const float inv = any ? 1.f / sum[m] : 0.f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[m][t][i] = any ? acc[m][t][i] * inv : 0.f;
+  }
+  const float *handed = reinterpret_cast<const float *>(smem) + (wave >> 1) * 32 * F::kWidth + lane;
+  if constexpr (kMaps == 1) {
+    // the second map's wave hands its results to the first one's
+    float *x = reinterpret_cast<float *>(smem) + (wave >> 1) * 32 * F::kWidth + lane;
+    tile_barrier();
+    if (map0) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(t * 16 + i) * 64] = acc[0][t][i];
+    }
+    tile_barrier();
+  }
+  if (row >= rows) return;
+  const float lam = a.lam[head];
+  T *o = static_cast<T *>(a.out) + clip * a.o_batch + query * a.o_pitch + static_cast<int64_t>(head) * 2 * a.d;
+  T *o2 = static_cast<T *>(a.out2) + ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;
+  struct alignas(4 * sizeof(T)) Four {
+    T v[4];
+  };
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = t * 32 + 8 * g + 4 * half;
+      if (col >= 2 * a.d) continue;
+      Four x, y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 4 * g + e;
+        const float second = kMaps == 2 ? acc[kMaps - 1][t][i] : map0 ? acc[0][t][i] : handed[(t * 16 + i) * 64];
+        x.v[e] = static_cast<T>(acc[0][t][i] - lam * second);
+        y.v[e] = static_cast<T>(second);
+      }
+      if (!map0) *reinterpret_cast<Four *>(o + col) = x;
+      if (a.out2 && map0 == kMaps % 2) *reinterpret_cast<Four *>(o2 + col) = y;
+    }
+  if (a.lse && half == 0) {
+    const int64_t at = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
+#pragma unroll
+    for (int m = 0; m < kMaps; ++m)
+      a.lse[(map0 + m) * static_cast<int64_t>(a.n) * a.hq * a.lq + at] = any ? top[m] + log2f(sum[m]) : INFINITY;
+  }
+}
+
+// Joins the splits of a call with few rows, in their order: one wave per row.
+template <typename T>
+__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a) {
+  const int rows = a.lq * a.group;
+  const int64_t r = blockIdx.x, total = static_cast<int64_t>(a.n) * a.hk * rows;
+  const int row = static_cast<int>(r % rows);
+  const int64_t pair = r / rows;
+  const int kvh = static_cast<int>(pair % a.hk), clip = static_cast<int>(pair / a.hk);
+  const int query = row / a.group, head = kvh * a.group + (row - query * a.group);
+  const bool in = query < clip_length(a.q_len, clip, a.lq);
+  const float *st = a.part + r * 4;
+  float top[2] = {-INFINITY, -INFINITY};
+  for (int s = 0; in && s < a.splits; ++s)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], st[s * total * 4 + 2 * m]);
+  const bool any = top[0] > -INFINITY;
+  float sum[2] = {0.f, 0.f};
+  for (int s = 0; any && s < a.splits; ++s)
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+      sum[m] += st[s * total * 4 + 2 * m + 1] * __builtin_amdgcn_exp2f(st[s * total * 4 + 2 * m] - top[m]);
+  const float lam = a.lam[head];
+  T *o = static_cast<T *>(a.out) + clip * a.o_batch + query * a.o_pitch + static_cast<int64_t>(head) * 2 * a.d;
+  T *o2 = a.out2 ? static_cast<T *>(a.out2) +
+                       ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d
+                 : nullptr;
+  const float *part = a.part + a.splits * total * 4 + r * 4 * a.d;
+  for (int col = threadIdx.x; col < 2 * a.d; col += 64) {
+    float v[2] = {0.f, 0.f};
+    for (int s = 0; any && s < a.splits; ++s) {
+      if (st[s * total * 4 + 1] == 0.f) continue;  // this split saw no key
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        v[m] += part[s * total * 4 * a.d + m * 2 * a.d + col] *
+                __builtin_amdgcn_exp2f(st[s * total * 4 + 2 * m] - top[m]);
+    }
+    const float second = any ? v[1] / sum[1] : 0.f;
+    o[col] = static_cast<T>(any ? v[0] / sum[0] - lam * second : 0.f);
+    if (o2) o2[col] = static_cast<T>(second);
+  }
+  if (a.lse && threadIdx.x < 2) {
+    const int m = threadIdx.x;
+    const int64_t at = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
+    a.lse[m * static_cast<int64_t>(a.n) * a.hq * a.lq + at] = any ? top[m] + log2f(sum[m]) : INFINITY;
+  }
+}
+
+template <typename T, int D, int ROWS, bool SPLIT>
+int fwd(const AttnArgs &a, hipStream_t s) {
+  using F = Fwd<T, D, ROWS>;
+  const int e = allow_lds<attn_fwd_kernel<T, D, ROWS, SPLIT>>(F::kLds);
+  if (e != hipSuccess) return e;
+  attn_fwd_kernel<T, D, ROWS, SPLIT><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
+  if (SPLIT)
+    attn_join_kernel<T><<<static_cast<unsigned>(static_cast<int64_t>(a.n) * a.hk * a.lq * a.group), 64, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+int fwd_shape(const AttnArgs &a, int rows, hipStream_t s) {
+  if (rows == 1) return a.splits > 1 ? fwd<T, D, 1, true>(a, s) : fwd<T, D, 1, false>(a, s);
+  return fwd<T, D, attn_row_groups(D), false>(a, s);
+}
+
+template <typename T>
+int fwd_type(const AttnArgs &a, int rows, hipStream_t s) {
+  if (a.d <= 32) return fwd_shape<T, 32>(a, rows, s);
+  if (a.d <= 64) return fwd_shape<T, 64>(a, rows, s);
+  return fwd_shape<T, 128>(a, rows, s);
+}
+
+}  // namespace
+
+int launch_attn_fwd(const AttnArgs &a, int dtype, int rows, void *stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == RT3D_F32) return fwd_type<float>(a, rows, s);
+  if (dtype == RT3D_BF16) return fwd_type<__bf16>(a, rows, s);
+  return fwd_type<_Float16>(a, rows, s);
+}
+
+}  // namespace rt3d

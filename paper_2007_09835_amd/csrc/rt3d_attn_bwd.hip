@@ -1,0 +1,448 @@
+// Differential attention on gfx950 (MI355X), backward.  With P_m the softmax maps,
+// A_m the row sums of P_m dP and dP = do v^T:
+//   dS_1 = P_1 (dP - A_1),  dS_2 = -lambda P_2 (dP - A_2),
+//   dq_m = scale dS_m k_m,  dk_m = scale dS_m^T q_m,  dv = (P_1 - lambda P_2)^T do,
+//   dlambda = -sum of P_2 dP.
+// The probabilities come back from the scores and the logarithms that the
+// forward pass left.  A_m = do . o_m is formed from o and the second map's output.
+// Two kernels, each owning what it sums, so no result depends on an order of
+// arrival: one walks the keys for its query rows, one the queries for its keys.
+
+#include "rt3d_attn.h"
+
+namespace rt3d {
+namespace {
+
+using namespace attn;
+
+template <typename T, int D, int WAVES>
+struct Dq {
+  static constexpr int kKeys = WAVES == 1 || D > 64 || sizeof(T) == 4 ? 32 : 64;
+  static constexpr int kThreads = 64 * WAVES;
+  using KV = Tile<T, D, kKeys, kThreads>;
+  static constexpr int kLds = 4 * KV::kBytes;
+  static constexpr int kMinWaves = sizeof(T) == 2 && D <= 64 ? 2 : 1;
+};
+
+// Rows of queries as in the forward pass (a lane holds a row): S^T = K Q^T and
+// dP^T = V dO^T leave dS^T where the product dQ^T += K^T dS^T takes it.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn_dq_kernel(AttnArgs a) {
+  using F = Dq<T, D, WAVES>;
+  using KV = typename F::KV;
+  constexpr int kKeys = F::kKeys;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  lds_char *lds = (lds_char *)smem;
+
+  int64_t id = logical_block(a.blocks);
+  if (id >= a.blocks) return;
+  const int tile = a.tiles - 1 - static_cast<int>(id % a.tiles);
+  id /= a.tiles;
+  const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
+  const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);
+  const int rows = a.lq * a.group, used = q_len * a.group;
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(static_cast<int>(threadIdx.x) >> 6);
+  const int first = (tile * WAVES + wave) * 32, row = first + (lane & 31);
+  const int query = row / a.group, head = kvh * a.group + (row - query * a.group);
+  const bool in = row < used;
+  const int limit = in ? visible(query, q_len, k_len, a.frame) : 0x7fffffff;
+  const int last_block = min(used, (tile + 1) * WAVES * 32) - 1, last_wave = min(used, first + 32) - 1;
+  const int end = last_block < tile * WAVES * 32 ? 0 : visible(last_block / a.group, q_len, k_len, a.frame);
+  const int wave_end = last_wave < first ? 0 : visible(last_wave / a.group, q_len, k_len, a.frame);
+  const int whole = last_wave < first ? 0 : visible(first / a.group, q_len, k_len, a.frame);
+
+  const int64_t map = static_cast<int64_t>(a.n) * a.hq * a.lq;
+  const int64_t stat = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
+  const float lam = in ? a.lam[head] : 0.f;
+  f32x16 acc[2][D / 32] = {};
+  float dl = 0.f;
+
+  if (end > 0) {
+    Frag<T> q[2][D / 16], g[2 * D / 16];
+    float lse[2] = {INFINITY, INFINITY}, mean[2] = {0.f, 0.f};
+    {
+      const T *p = static_cast<const T *>(a.q) + clip * a.q_batch + query * a.q_pitch +
+                   static_cast<int64_t>(head) * 2 * a.d;
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+          const int col = s * 16 + 8 * half;
+          q[m][s] = in && col < a.d ? load_frag(p + m * a.d + col) : Frag<T>{};
+        }
+      const T *go = static_cast<const T *>(a.d_o) + clip * a.do_batch + query * a.do_pitch +
+                    static_cast<int64_t>(head) * 2 * a.d;
+      const T *o = static_cast<const T *>(a.o) + clip * a.o_batch + query * a.o_pitch +
+                   static_cast<int64_t>(head) * 2 * a.d;
+      const T *o2 = static_cast<const T *>(a.o2) +
+                    ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;
+#pragma unroll
+      for (int s = 0; s < 2 * D / 16; ++s) {
+        const int col = s * 16 + 8 * half;
+        const bool get = in && col < 2 * a.d;
+        g[s] = get ? load_frag(go + col) : Frag<T>{};
+        const Frag<T> x = get ? load_frag(o + col) : Frag<T>{}, y = get ? load_frag(o2 + col) : Frag<T>{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          mean[0] += static_cast<float>(g[s][e]) * static_cast<float>(x[e]);
+          mean[1] += static_cast<float>(g[s][e]) * static_cast<float>(y[e]);
+        }
+      }
+      mean[1] = half_sum(mean[1]);
+      mean[0] = half_sum(mean[0]) + lam * mean[1];
+      if (in) {
+        lse[0] = a.lse[stat];
+        lse[1] = a.lse[map + stat];
+        if (half == 0) {
+          a.rowstat[stat] = mean[0];
+          a.rowstat[map + stat] = mean[1];
+        }
+      }
+    }
+    unsigned k_off[KV::kLoads], v_off[KV::kLoads];
+    KV::template offsets<true>(a.d, a.k_pitch, k_off);
+    KV::template offsets<false>(a.d, a.v_pitch, v_off);
+    const T *k = static_cast<const T *>(a.k) + clip * a.k_batch + static_cast<int64_t>(kvh) * 2 * a.d;
+    const T *v = static_cast<const T *>(a.v) + clip * a.v_batch + static_cast<int64_t>(kvh) * 2 * a.d;
+    auto stage = [&](int key, int buf) {
+      const int n = min(kKeys, k_len - key);
+      KV::stage(k + key * a.k_pitch, n, a.d, a.k_pitch, k_off, lds + buf * 2 * KV::kBytes);
+      KV::stage(v + key * a.v_pitch, n, a.d, a.v_pitch, v_off, lds + (buf * 2 + 1) * KV::kBytes);
+    };
+    stage(0, 0);
+    int buf = 0;
+    for (int key = 0; key < end; key += kKeys, buf ^= 1) {
+      tile_barrier();
+      if (key + kKeys < end) stage(key + kKeys, buf ^ 1);
+      if (key >= wave_end) continue;
+      const lds_char *kt = lds + buf * 2 * KV::kBytes, *vt = kt + KV::kBytes;
+      const bool masked = key + kKeys > whole;
+      for (int j = 0; j < kKeys; j += 32) {
+        f32x16 dp = {};
+#pragma unroll
+        for (int i = 0; i < 2 * D / 16; ++i) dp = Mma<T>::run(KV::along(vt, j, i * 16), g[i], dp);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          f32x16 s = {};
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) s = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s);
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (key + j + result_row(i, half) >= limit) s[i] = -INFINITY;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -lse[m]));
+            if (m) dl += p * dp[i];
+            s[i] = p * (dp[i] - mean[m]);
+          }
+          // the softmax of a single key does not move (its row sum is exact here)
+          if (masked && limit <= 1) s = f32x16{};
+          const Frag<T> lo = pack<T>(s, 0), hi = pack<T>(s, 8);
+#pragma unroll
+          for (int t = 0; t < D / 32; ++t) {
+            acc[m][t] = Mma<T>::run(KV::across(kt, j, m * D + t * 32), lo, acc[m][t]);
+            acc[m][t] = Mma<T>::run(KV::across(kt, j + 16, m * D + t * 32), hi, acc[m][t]);
+          }
+        }
+      }
+    }
+  }
+  if (row >= rows) return;
+  dl = half_sum(dl);
+  if (half == 0) {
+    a.rowstat[2 * map + stat] = dl;
+    if (end <= 0) a.rowstat[stat] = a.rowstat[map + stat] = 0.f;
+  }
+  if (!a.dq) return;
+  T *dq = static_cast<T *>(a.dq) + clip * a.dq_batch + query * a.dq_pitch + static_cast<int64_t>(head) * 2 * a.d;
+  struct alignas(4 * sizeof(T)) Four {
+    T v[4];
+  };
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const float by = m ? -lam * a.scale : a.scale;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int col = t * 32 + 8 * r + 4 * half;
+        if (col >= a.d) continue;
+        Four x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.v[e] = static_cast<T>(acc[m][t][4 * r + e] * by);
+        *reinterpret_cast<Four *>(dq + m * a.d + col) = x;
+      }
+  }
+}
+
+// A lane holds a key: S = Q K^T and dP = dO V^T with the keys and values in
+// registers leave P and dS where dV^T += dO^T P and dK^T += Q^T dS take them.  The
+// heads of a key head's group follow one another and add to the same results.
+template <typename T, int D, int WAVES>
+struct Dkv {
+  static constexpr int kRows = 32;
+  static constexpr int kThreads = 64 * WAVES;
+  using Q = Tile<T, D, kRows, kThreads>;
+  static constexpr int kStat = 4 * 64 * 4;  // logarithms and row sums of the tile's rows
+  static constexpr int kLds = 2 * (2 * Q::kBytes + kStat);
+  static constexpr int kMinWaves = sizeof(T) == 2 && D <= 64 ? 2 : 1;
+  // 32-bit keys and values of 128 and 256 columns beside their gradients pass the
+  // register file: they are read again for every tile (from L1).
+  static constexpr bool kHold = sizeof(T) == 2 || D <= 64;
+};
+
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void attn_dkv_kernel(AttnArgs a) {
+  using F = Dkv<T, D, WAVES>;
+  using Q = typename F::Q;
+  constexpr int kRows = F::kRows;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  lds_char *lds = (lds_char *)smem;
+
+  int64_t id = logical_block(a.blocks);
+  if (id >= a.blocks) return;
+  const int tile = static_cast<int>(id % a.tiles);  // keys that most queries see first
+  id /= a.tiles;
+  const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
+  const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(static_cast<int>(threadIdx.x) >> 6);
+  const int key_block = tile * WAVES * 32, key_wave = key_block + wave * 32, key = key_wave + (lane & 31);
+  const bool in = key < k_len;
+  // first query that sees a key: the one that stands where the key's frame begins
+  auto first_query = [&](int k) { return a.frame ? k / a.frame * a.frame - (k_len - q_len) : 0; };
+  const int from = first_query(key), from_wave = first_query(key_wave);
+  // queries whose softmax has one key: all of a clip with one, or the one that
+  // stands at the first key where every token is a frame (none if negative)
+  const bool single_all = k_len == 1;
+  const int single = a.frame == 1 ? q_len - k_len : -1;
+
+  f32x16 dk[2][D / 32] = {}, dv[2 * D / 32] = {};
+  const int begin = max(0, first_query(key_block)) / kRows * kRows;
+
+  if (key_block < k_len && begin < q_len) {
+    const T *k = static_cast<const T *>(a.k) + clip * a.k_batch + (in ? key : 0) * a.k_pitch +
+                 static_cast<int64_t>(kvh) * 2 * a.d;
+    const T *v = static_cast<const T *>(a.v) + clip * a.v_batch + (in ? key : 0) * a.v_pitch +
+                 static_cast<int64_t>(kvh) * 2 * a.d;
+    auto key_frag = [&](int m, int s) {
+      const int col = s * 16 + 8 * half;
+      return in && col < a.d ? load_frag(k + m * a.d + col) : Frag<T>{};
+    };
+    auto value_frag = [&](int s) {
+      const int col = s * 16 + 8 * half;
+      return in && col < 2 * a.d ? load_frag(v + col) : Frag<T>{};
+    };
+    Frag<T> kf[F::kHold ? 2 : 1][F::kHold ? D / 16 : 1], vf[F::kHold ? 2 * D / 16 : 1];
+    if constexpr (F::kHold) {
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) kf[0][s] = key_frag(0, s), kf[1][s] = key_frag(1, s);
+#pragma unroll
+      for (int s = 0; s < 2 * D / 16; ++s) vf[s] = value_frag(s);
+    }
+    unsigned q_off[Q::kLoads], g_off[Q::kLoads];
+    Q::template offsets<true>(a.d, a.q_pitch, q_off);
+    Q::template offsets<false>(a.d, a.do_pitch, g_off);
+    const int64_t map = static_cast<int64_t>(a.n) * a.hq * a.lq;
+    const int per_head = (q_len - begin + kRows - 1) / kRows, total = per_head * a.group;
+    const T *q = static_cast<const T *>(a.q) + clip * a.q_batch;
+    const T *go = static_cast<const T *>(a.d_o) + clip * a.do_batch;
+    // tile t: rows of head t / per_head from begin + t % per_head * kRows on
+    int st_head = 0, st_row = begin;  // of the tile to be staged next
+    auto stage = [&](int buf) {
+      const int head = kvh * a.group + st_head, n = min(kRows, q_len - st_row);
+      lds_char *to = lds + buf * (2 * Q::kBytes + F::kStat);
+      Q::stage(q + st_row * a.q_pitch + static_cast<int64_t>(head) * 2 * a.d, n, a.d, a.q_pitch, q_off, to);
+      Q::stage(go + st_row * a.do_pitch + static_cast<int64_t>(head) * 2 * a.d, n, a.d, a.do_pitch, g_off,
+               to + Q::kBytes);
+      // logarithms of both maps, then row sums: one row of 64 lanes each
+#pragma unroll
+      for (int i = 0; i < 4 / (WAVES < 4 ? WAVES : 4); ++i) {
+        const int which = i * WAVES + wave;
+        const int64_t at = (which & 1) * map + (static_cast<int64_t>(clip) * a.hq + head) * a.lq + st_row;
+        const float *src = (which & 2 ? a.rowstat : a.lse) + at;
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(src), 0, n * 4, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            r, (__attribute__((address_space(3))) void *)(to + 2 * Q::kBytes + which * 256), 4, lane * 4, 0, 0, 0);
+      }
+      if ((st_row += kRows) >= q_len) {
+        st_row = begin;
+        ++st_head;
+      }
+    };
+    stage(0);
+    int buf = 0, head = 0, row0 = begin;
+    for (int t = 0; t < total; ++t, buf ^= 1) {
+      tile_barrier();
+      if (t + 1 < total) stage(buf ^ 1);
+      const float lam = a.lam[kvh * a.group + head];
+      const int at = row0;
+      if ((row0 += kRows) >= q_len) {
+        row0 = begin;
+        ++head;
+      }
+      // no row of the tile sees a key of this wave, or it has none
+      if (at + kRows <= from_wave || key_wave >= k_len) continue;
+      const lds_char *qt = lds + buf * (2 * Q::kBytes + F::kStat), *gt = qt + Q::kBytes, *st = gt + Q::kBytes;
+      // some pair of the tile is masked, or some row has a single key
+      const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
+      const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
+      f32x16 dp = {}, pv;
+#pragma unroll
+      for (int i = 0; i < 2 * D / 16; ++i) {
+        Frag<T> b;
+        if constexpr (F::kHold) b = vf[i];
+        else b = value_frag(i);
+        dp = Mma<T>::run(Q::along(gt, 0, i * 16), b, dp);
+      }
+      Frag<T> ds[2][2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        f32x16 s = {};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          Frag<T> b;
+          if constexpr (F::kHold) b = kf[m][i];
+          else b = key_frag(m, i);
+          s = Mma<T>::run(Q::along(qt, 0, m * D + i * 16), b, s);
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (at + result_row(i, half) < from) s[i] = -INFINITY;
+        }
+        const float by = m ? -lam : 1.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x4 lse = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(
+              st + m * 256 + (8 * r + 4 * half) * 4);
+          const f32x4 mean = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(
+              st + (2 + m) * 256 + (8 * r + 4 * half) * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = 4 * r + e;
+            const float p = by * __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -lse[e]));
+            pv[i] = m ? pv[i] + p : p;
+            s[i] = p * (dp[i] - mean[e]);
+          }
+        }
+        if (lone) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (single_all || at + result_row(i, half) == single) s[i] = 0.f;
+        }
+        ds[m][0] = pack<T>(s, 0);
+        ds[m][1] = pack<T>(s, 8);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const Frag<T> p = pack<T>(pv, 8 * h);
+#pragma unroll
+        for (int c = 0; c < 2 * D / 32; ++c) dv[c] = Mma<T>::run(Q::across(gt, 16 * h, c * 32), p, dv[c]);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c)
+            dk[m][c] = Mma<T>::run(Q::across(qt, 16 * h, m * D + c * 32), ds[m][h], dk[m][c]);
+      }
+    }
+  }
+  if (key >= a.lk) return;
+  struct alignas(4 * sizeof(T)) Four {
+    T v[4];
+  };
+  if (a.dk) {
+    T *p = static_cast<T *>(a.dk) + clip * a.dk_batch + key * a.dk_pitch + static_cast<int64_t>(kvh) * 2 * a.d;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int col = t * 32 + 8 * r + 4 * half;
+          if (col >= a.d) continue;
+          Four x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.v[e] = static_cast<T>(in ? dk[m][t][4 * r + e] * a.scale : 0.f);
+          *reinterpret_cast<Four *>(p + m * a.d + col) = x;
+        }
+  }
+  if (a.dv) {
+    T *p = static_cast<T *>(a.dv) + clip * a.dv_batch + key * a.dv_pitch + static_cast<int64_t>(kvh) * 2 * a.d;
+#pragma unroll
+    for (int t = 0; t < 2 * D / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int col = t * 32 + 8 * r + 4 * half;
+        if (col >= 2 * a.d) continue;
+        Four x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.v[e] = static_cast<T>(in ? dv[t][4 * r + e] : 0.f);
+        *reinterpret_cast<Four *>(p + col) = x;
+      }
+  }
+}
+
+// dlambda of a head: its rows' sums, in a fixed order.
+__global__ __launch_bounds__(256) void attn_dlam_kernel(AttnArgs a) {
+  __shared__ float lds[256];
+  const int head = blockIdx.x;
+  const float *p = a.rowstat + 2 * static_cast<int64_t>(a.n) * a.hq * a.lq;
+  float s = 0.f;
+  for (int clip = 0; clip < a.n; ++clip) {
+    const float *r = p + (static_cast<int64_t>(clip) * a.hq + head) * a.lq;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < a.lq; i += 256) s += r[i];
+  }
+  lds[threadIdx.x] = s;
+  __syncthreads();
+  for (int w = 128; w > 0; w >>= 1) {
+    if (static_cast<int>(threadIdx.x) < w) lds[threadIdx.x] += lds[threadIdx.x + w];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) a.dlam[head] = 0.f - lds[0];
+}
+
+template <typename T, int D, int WAVES>
+int bwd(AttnArgs a, hipStream_t s) {
+  using A = Dq<T, D, WAVES>;
+  using B = Dkv<T, D, WAVES>;
+  const int64_t pairs = static_cast<int64_t>(a.n) * a.hk;
+  int e = allow_lds<attn_dq_kernel<T, D, WAVES>>(A::kLds);
+  if (e == hipSuccess) e = allow_lds<attn_dkv_kernel<T, D, WAVES>>(B::kLds);
+  if (e != hipSuccess) return e;
+  a.tiles = (a.lq * a.group + 32 * WAVES - 1) / (32 * WAVES);
+  a.blocks = pairs * a.tiles;
+  if (a.blocks) attn_dq_kernel<T, D, WAVES><<<grid_of(a.blocks), A::kThreads, A::kLds, s>>>(a);
+  a.tiles = (a.lk + 32 * WAVES - 1) / (32 * WAVES);
+  a.blocks = pairs * a.tiles;
+  if (a.blocks && (a.dk || a.dv))
+    attn_dkv_kernel<T, D, WAVES><<<grid_of(a.blocks), B::kThreads, B::kLds, s>>>(a);
+  if (a.dlam) attn_dlam_kernel<<<a.hq, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+int bwd_waves(const AttnArgs &a, hipStream_t s) {
+  return bwd<T, D, 4>(a, s);
+}
+
+template <typename T>
+int bwd_type(const AttnArgs &a, hipStream_t s) {
+  if (a.d <= 32) return bwd_waves<T, 32>(a, s);
+  if (a.d <= 64) return bwd_waves<T, 64>(a, s);
+  return bwd_waves<T, 128>(a, s);
+}
+
+}  // namespace
+
+int launch_attn_bwd(const AttnArgs &a, int dtype, void *stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == RT3D_F32) return bwd_type<float>(a, s);
+  if (dtype == RT3D_BF16) return bwd_type<__bf16>(a, s);
+  return bwd_type<_Float16>(a, s);
+}
+
+}  // namespace rt3d

@@ -22,9 +22,8 @@
 #include "rt3d_internal.h"
 
 namespace rt3d {
-namespace {
 
-thread_local std::string g_detail;
+static thread_local std::string g_detail;
 
 rt3d_status fail(rt3d_status s, const char *fmt, ...) {
   char buf[512];
@@ -40,6 +39,8 @@ rt3d_status ok() {
   g_detail.clear();
   return RT3D_OK;
 }
+
+namespace {
 
 int esize_of(int dtype) { return dtype == RT3D_F32 ? 4 : 2; }
 

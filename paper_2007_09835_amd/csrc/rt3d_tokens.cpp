@@ -1,0 +1,428 @@
+// Host side of librt3d's token operators: argument validation, launch rules and
+// the C entry points declared in include/rt3d.h.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "rt3d_tokens.h"
+
+namespace rt3d {
+namespace {
+
+constexpr int64_t kMaxBlocks = (1ll << 31) - 16;
+constexpr int kMaxNormColumns = 1 << 20;
+constexpr int64_t kMaxPitch = 1 << 22;   // elements: a tile's rows stay within 2^31 bytes
+constexpr int kMaxLength = 1 << 30;
+
+bool known_dtype(int dtype) { return dtype == RT3D_F32 || dtype == RT3D_BF16 || dtype == RT3D_F16; }
+int esize(int dtype) { return dtype == RT3D_F32 ? 4 : 2; }
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+rt3d_status launched(int e) {
+  if (e != hipSuccess)
+    return fail(RT3D_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(static_cast<hipError_t>(e)));
+  return ok();
+}
+
+// ---------------------------------------------------------------------------
+// Layer norm
+// ---------------------------------------------------------------------------
+
+rt3d_status check_norm(const rt3d_norm_desc *d) {
+  if (!d) return fail(RT3D_ERR_INVALID_ARG, "desc is NULL");
+  if (d->rows < 0) return fail(RT3D_ERR_INVALID_ARG, "rows must be non-negative");
+  if (d->c <= 0) return fail(RT3D_ERR_INVALID_ARG, "c must be positive");
+  if (!known_dtype(d->dtype)) return fail(RT3D_ERR_INVALID_ARG, "unknown dtype %d", d->dtype);
+  if (!(d->eps > 0.f) || !std::isfinite(d->eps))
+    return fail(RT3D_ERR_INVALID_ARG, "eps must be finite and > 0");
+  if ((d->x_pitch && d->x_pitch < d->c) || (d->y_pitch && d->y_pitch < d->c))
+    return fail(RT3D_ERR_INVALID_ARG, "pitches must be 0 or at least c");
+  if (d->c > kMaxNormColumns) return fail(RT3D_ERR_UNSUPPORTED, "rows of more than %d channels", kMaxNormColumns);
+  if (static_cast<double>(d->rows) * static_cast<double>(std::max({d->x_pitch, d->y_pitch, static_cast<int64_t>(d->c)})) >
+      9.0e18 / 4)
+    return fail(RT3D_ERR_UNSUPPORTED, "rows times pitch passes 64 bits");
+  return RT3D_OK;
+}
+
+NormArgs norm_args(const rt3d_norm_desc *d) {
+  NormArgs a{};
+  a.rows = d->rows;
+  a.c = d->c;
+  a.eps = d->eps;
+  a.x_pitch = d->x_pitch ? d->x_pitch : d->c;
+  a.y_pitch = d->y_pitch ? d->y_pitch : d->c;
+  a.blocks = layernorm_bwd_blocks(d->rows, d->c);
+  return a;
+}
+
+uint64_t norm_workspace(const rt3d_norm_desc *d) {
+  return static_cast<uint64_t>(layernorm_bwd_blocks(d->rows, d->c)) * 2 * d->c * sizeof(float);
+}
+
+// ---------------------------------------------------------------------------
+// Rotation by positions
+// ---------------------------------------------------------------------------
+
+rt3d_status check_rope(const rt3d_rope_desc *d) {
+  if (!d) return fail(RT3D_ERR_INVALID_ARG, "desc is NULL");
+  if (d->n < 0 || d->t < 0) return fail(RT3D_ERR_INVALID_ARG, "n and t must be non-negative");
+  if (d->h <= 0 || d->w <= 0 || d->vecs <= 0) return fail(RT3D_ERR_INVALID_ARG, "h, w and vecs must be positive");
+  if (d->d <= 0 || d->d % 2) return fail(RT3D_ERR_INVALID_ARG, "d must be positive and even");
+  if (d->dt < 0 || d->dh < 0 || d->dw < 0 || d->dt % 2 || d->dh % 2 || d->dw % 2)
+    return fail(RT3D_ERR_INVALID_ARG, "sections must be non-negative and even");
+  if (static_cast<int64_t>(d->dt) + d->dh + d->dw > d->d)
+    return fail(RT3D_ERR_INVALID_ARG, "sections pass the vector's %d channels", d->d);
+  if (!known_dtype(d->dtype)) return fail(RT3D_ERR_INVALID_ARG, "unknown dtype %d", d->dtype);
+  if (d->flags & ~(RT3D_ROPE_HALVES | RT3D_ROPE_INVERSE)) return fail(RT3D_ERR_INVALID_ARG, "unknown flags");
+  if (!(d->base > 0.f) || !std::isfinite(d->base)) return fail(RT3D_ERR_INVALID_ARG, "base must be finite and > 0");
+  if (d->t0 < 0 || static_cast<int64_t>(d->t0) + d->t > 0x7fffffffll)
+    return fail(RT3D_ERR_INVALID_ARG, "positions t0 .. t0 + t must lie in 0 .. 2^31 - 1");
+  const int64_t row = static_cast<int64_t>(d->vecs) * d->d;
+  for (const rt3d_rows *r : {&d->x, &d->y}) {
+    if (r->pitch && r->pitch < row) return fail(RT3D_ERR_INVALID_ARG, "pitches must be 0 or at least vecs * d");
+    if (r->batch < 0) return fail(RT3D_ERR_INVALID_ARG, "batch strides must be non-negative");
+  }
+  if (static_cast<double>(d->h) * d->w * std::max(d->t, 1) > 2.0e9)
+    return fail(RT3D_ERR_UNSUPPORTED, "more than 2e9 tokens in a clip");
+  return RT3D_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Differential attention
+// ---------------------------------------------------------------------------
+
+struct Shape {
+  int64_t q_row, k_row;  // elements of a token's queries (and outputs), keys (and values)
+  int group;
+};
+
+rt3d_status check_rows(const rt3d_rows &r, int64_t row, int64_t len, int es, bool out, const char *what) {
+  if (r.pitch && r.pitch < row) return fail(RT3D_ERR_INVALID_ARG, "%s: pitch below %lld", what, static_cast<long long>(row));
+  if (r.batch < 0) return fail(RT3D_ERR_INVALID_ARG, "%s: batch stride is negative", what);
+  const int64_t pitch = r.pitch ? r.pitch : row;
+  if (out && r.batch && r.batch < (std::max<int64_t>(len, 1) - 1) * pitch + row)
+    return fail(RT3D_ERR_INVALID_ARG, "%s: clips overlap", what);
+  if (pitch >= kMaxPitch) return fail(RT3D_ERR_UNSUPPORTED, "%s: a token pitch of 2^22 elements or more", what);
+  if (pitch * es % 16 || r.batch * es % 16)
+    return fail(RT3D_ERR_UNSUPPORTED, "%s: strides must be multiples of 16 bytes", what);
+  return RT3D_OK;
+}
+
+rt3d_status check_attn(const rt3d_diffattn_desc *d, bool backward, Shape &s) {
+  if (!d) return fail(RT3D_ERR_INVALID_ARG, "desc is NULL");
+  if (d->n < 0 || d->lq < 0 || d->lk < 0) return fail(RT3D_ERR_INVALID_ARG, "n, lq and lk must be non-negative");
+  if (d->hq <= 0 || d->hk <= 0 || d->hq % d->hk)
+    return fail(RT3D_ERR_INVALID_ARG, "hq must be a positive multiple of hk");
+  if (d->d <= 0) return fail(RT3D_ERR_INVALID_ARG, "d must be positive");
+  if (!known_dtype(d->dtype)) return fail(RT3D_ERR_INVALID_ARG, "unknown dtype %d", d->dtype);
+  if (d->frame < 0) return fail(RT3D_ERR_INVALID_ARG, "frame must be non-negative");
+  if (!(d->scale >= 0.f) || !std::isfinite(d->scale))
+    return fail(RT3D_ERR_INVALID_ARG, "scale must be finite and >= 0");
+  if (d->d % 8 || d->d > 128) return fail(RT3D_ERR_UNSUPPORTED, "d must be a multiple of 8 up to 128, got %d", d->d);
+  s.group = d->hq / d->hk;
+  if (d->lq >= kMaxLength || d->lk >= kMaxLength || d->frame >= kMaxLength ||
+      static_cast<int64_t>(d->lq) * s.group >= kMaxLength)
+    return fail(RT3D_ERR_UNSUPPORTED, "lengths (times hq / hk) must be below 2^30");
+  const double rows = static_cast<double>(d->n) * d->hk * (static_cast<double>(d->lq) * s.group + d->lk + 64);
+  if (rows >= static_cast<double>(kMaxBlocks)) return fail(RT3D_ERR_UNSUPPORTED, "more than 2^31 rows");
+  s.q_row = 2ll * d->hq * d->d;
+  s.k_row = 2ll * d->hk * d->d;
+  const int es = esize(d->dtype);
+  rt3d_status st = RT3D_OK;
+  auto rows_of = [&](const rt3d_rows &r, int64_t row, int len, bool out, const char *what) {
+    if (st == RT3D_OK) st = check_rows(r, row, len, es, out, what);
+  };
+  rows_of(d->q, s.q_row, d->lq, false, "q");
+  rows_of(d->k, s.k_row, d->lk, false, "k");
+  rows_of(d->v, s.k_row, d->lk, false, "v");
+  rows_of(d->o, s.q_row, d->lq, true, "o");
+  if (backward) {
+    rows_of(d->d_o, s.q_row, d->lq, false, "d_o");
+    rows_of(d->dq, s.q_row, d->lq, true, "dq");
+    rows_of(d->dk, s.k_row, d->lk, true, "dk");
+    rows_of(d->dv, s.k_row, d->lk, true, "dv");
+  }
+  return st;
+}
+
+void put_rows(const rt3d_rows &r, int64_t row, int64_t len, int64_t &pitch, int64_t &batch) {
+  pitch = r.pitch ? r.pitch : row;
+  batch = r.batch ? r.batch : len * pitch;
+}
+
+AttnArgs attn_args(const rt3d_diffattn_desc *d, const Shape &s) {
+  AttnArgs a{};
+  a.n = d->n;
+  a.lq = d->lq;
+  a.lk = d->lk;
+  a.hq = d->hq;
+  a.hk = d->hk;
+  a.d = d->d;
+  a.group = s.group;
+  a.frame = d->frame;
+  a.scale = d->scale > 0.f ? d->scale : 1.f / std::sqrt(static_cast<float>(d->d));
+  a.scale2 = a.scale * 1.44269504088896340736f;
+  put_rows(d->q, s.q_row, d->lq, a.q_pitch, a.q_batch);
+  put_rows(d->k, s.k_row, d->lk, a.k_pitch, a.k_batch);
+  put_rows(d->v, s.k_row, d->lk, a.v_pitch, a.v_batch);
+  put_rows(d->o, s.q_row, d->lq, a.o_pitch, a.o_batch);
+  put_rows(d->d_o, s.q_row, d->lq, a.do_pitch, a.do_batch);
+  put_rows(d->dq, s.q_row, d->lq, a.dq_pitch, a.dq_batch);
+  put_rows(d->dk, s.k_row, d->lk, a.dk_pitch, a.dk_batch);
+  put_rows(d->dv, s.k_row, d->lk, a.dv_pitch, a.dv_batch);
+  return a;
+}
+
+// Launch of a forward call: groups of 32 rows of a workgroup and splits of the keys.
+struct FwdPlan {
+  int row_groups, tiles, splits, span;
+  int64_t blocks;
+  uint64_t bytes;  // workspace
+};
+
+constexpr int kFillBlocks = 512;     // two workgroups of four waves on each of 256 CUs
+constexpr int kSplitBlocks = 2048;   // single waves, when keys are split
+constexpr int kSplitKeys = 256;      // least keys of a split
+
+FwdPlan fwd_plan(const rt3d_diffattn_desc *d, const Shape &s, uint64_t workspace) {
+  FwdPlan p{};
+  const int64_t rows = static_cast<int64_t>(d->lq) * s.group, pairs = static_cast<int64_t>(d->n) * d->hk;
+  const int most = attn_row_groups(d->d);
+  auto tiles = [&](int groups) { return static_cast<int>((rows + 32 * groups - 1) / (32 * groups)); };
+  p.splits = 1;
+  p.span = d->lk;
+  p.row_groups = pairs * tiles(most) >= kFillBlocks ? most : 1;
+  p.tiles = tiles(p.row_groups);
+  p.blocks = pairs * p.tiles;
+  if (p.row_groups == 1 && p.blocks > 0) {
+    const uint64_t one = static_cast<uint64_t>(pairs * rows) * (4 + 4 * d->d) * sizeof(float);
+    int64_t splits = std::min<int64_t>(kSplitBlocks / p.blocks, d->lk / kSplitKeys);
+    splits = std::min<int64_t>(splits, static_cast<int64_t>(workspace / std::max<uint64_t>(one, 1)));
+    if (splits > 1) {
+      p.span = static_cast<int>(((d->lk + splits - 1) / splits + 31) / 32 * 32);
+      p.splits = (d->lk + p.span - 1) / p.span;
+      p.blocks *= p.splits;
+      p.bytes = one * p.splits;
+    }
+  }
+  return p;
+}
+
+uint64_t bwd_workspace(const rt3d_diffattn_desc *d) {
+  return 3ull * d->n * d->hq * d->lq * sizeof(float);
+}
+
+}  // namespace
+}  // namespace rt3d
+
+using namespace rt3d;
+
+extern "C" {
+
+rt3d_status rt3d_layernorm_fwd(const rt3d_norm_desc *d, const void *x, const float *gamma, const float *beta,
+                               void *y, float *mean, float *rstd, void *stream) {
+  const rt3d_status st = check_norm(d);
+  if (st != RT3D_OK) return st;
+  if (d->rows == 0) return ok();
+  if (!x || !y) return fail(RT3D_ERR_INVALID_ARG, "x and y must be non-NULL");
+  const int es = esize(d->dtype);
+  if (!aligned(x, es) || !aligned(y, es) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) ||
+      !aligned(rstd, 4))
+    return fail(RT3D_ERR_INVALID_ARG, "pointers must be aligned to their element size");
+  NormArgs a = norm_args(d);
+  a.x = x;
+  a.y = y;
+  a.gamma = gamma;
+  a.beta = beta;
+  a.mean = mean;
+  a.rstd = rstd;
+  return launched(launch_layernorm_fwd(a, d->dtype, stream));
+}
+
+rt3d_status rt3d_layernorm_bwd_workspace_size(const rt3d_norm_desc *d, uint64_t *bytes) {
+  const rt3d_status st = check_norm(d);
+  if (st != RT3D_OK) return st;
+  if (!bytes) return fail(RT3D_ERR_INVALID_ARG, "bytes must be non-NULL");
+  *bytes = norm_workspace(d);
+  return ok();
+}
+
+rt3d_status rt3d_layernorm_bwd(const rt3d_norm_desc *d, const void *x, const void *dy, const float *gamma,
+                               const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta,
+                               void *workspace, uint64_t workspace_bytes, void *stream) {
+  const rt3d_status st = check_norm(d);
+  if (st != RT3D_OK) return st;
+  const bool weights = dgamma || dbeta;
+  if (!dx && !weights) return ok();
+  if (d->rows > 0 && (!x || !dy || !mean || !rstd))
+    return fail(RT3D_ERR_INVALID_ARG, "x, dy, mean and rstd must be non-NULL");
+  const int es = esize(d->dtype);
+  if (!aligned(x, es) || !aligned(dy, es) || !aligned(dx, es) || !aligned(gamma, 4) || !aligned(mean, 4) ||
+      !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4) || !aligned(workspace, 4))
+    return fail(RT3D_ERR_INVALID_ARG, "pointers must be aligned to their element size");
+  if (weights && (!workspace || workspace_bytes < norm_workspace(d)))
+    return fail(RT3D_ERR_BUFFER_TOO_SMALL, "dgamma and dbeta need %llu bytes of workspace, got %llu",
+                static_cast<unsigned long long>(norm_workspace(d)),
+                static_cast<unsigned long long>(workspace ? workspace_bytes : 0));
+  if (d->rows == 0 && !weights) return ok();
+  NormArgs a = norm_args(d);
+  a.x = x;
+  a.dy = dy;
+  a.gamma = gamma;
+  a.mean = const_cast<float *>(mean);
+  a.rstd = const_cast<float *>(rstd);
+  a.dx = dx;
+  a.dgamma = dgamma;
+  a.dbeta = dbeta;
+  a.partial = weights ? static_cast<float *>(workspace) : nullptr;
+  return launched(launch_layernorm_bwd(a, d->dtype, stream));
+}
+
+rt3d_status rt3d_rope3d(const rt3d_rope_desc *d, const void *x, const int32_t *pos, void *y, void *stream) {
+  const rt3d_status st = check_rope(d);
+  if (st != RT3D_OK) return st;
+  RopeArgs a{};
+  a.tokens = static_cast<int64_t>(d->t) * d->h * d->w;
+  if (d->n == 0 || a.tokens == 0) return ok();
+  if (!x || !y) return fail(RT3D_ERR_INVALID_ARG, "x and y must be non-NULL");
+  const int es = esize(d->dtype);
+  if (!aligned(x, es) || !aligned(y, es) || !aligned(pos, 4))
+    return fail(RT3D_ERR_INVALID_ARG, "pointers must be aligned to their element size");
+  a.x = x;
+  a.y = y;
+  a.pos = pos;
+  put_rows(d->x, static_cast<int64_t>(d->vecs) * d->d, a.tokens, a.x_pitch, a.x_batch);
+  put_rows(d->y, static_cast<int64_t>(d->vecs) * d->d, a.tokens, a.y_pitch, a.y_batch);
+  if (d->n > 1 && a.y_batch < (a.tokens - 1) * a.y_pitch + static_cast<int64_t>(d->vecs) * d->d)
+    return fail(RT3D_ERR_INVALID_ARG, "clips of y overlap");
+  if (x == y && (a.x_pitch != a.y_pitch || a.x_batch != a.y_batch))
+    return fail(RT3D_ERR_INVALID_ARG, "a rotation in place needs one layout");
+  a.base_log2 = std::log2(static_cast<double>(d->base));
+  a.n = d->n;
+  a.h = d->h;
+  a.w = d->w;
+  a.vecs = d->vecs;
+  a.d = d->d;
+  a.size[0] = d->dt;
+  a.size[1] = d->dh;
+  a.size[2] = d->dw;
+  a.t0 = d->t0;
+  a.inverse = d->flags & RT3D_ROPE_INVERSE ? 1 : 0;
+  const int halves = d->flags & RT3D_ROPE_HALVES ? 1 : 0;
+  // The widest access (16 bytes at most) that every run of a thread allows.
+  int pairs = halves ? 16 / es : 8 / es;
+  const int rest = d->d - d->dt - d->dh - d->dw;
+  auto fits = [&](int p) {
+    const int run = halves ? p : 2 * p;  // elements of an access
+    if (d->d % run || a.x_pitch % run || a.y_pitch % run || a.x_batch % run || a.y_batch % run) return false;
+    if (!aligned(x, run * es) || !aligned(y, run * es)) return false;
+    if (!halves) return d->d % (2 * p) == 0;
+    return d->dt / 2 % p == 0 && d->dh / 2 % p == 0 && d->dw / 2 % p == 0 && rest / 2 % p == 0;
+  };
+  while (pairs > 1 && !fits(pairs)) pairs /= 2;
+  if (!fits(pairs)) return fail(RT3D_ERR_UNSUPPORTED, "pairs of neighbours need strides of whole pairs");
+  a.slots = d->d / 2 / pairs;
+  const int64_t base = static_cast<int64_t>(d->n) * a.tokens * a.slots;
+  constexpr int64_t kThreads = 512 * 1024;  // two waves of threads for every SIMD's eight
+  a.chunks = static_cast<int>(std::min<int64_t>(d->vecs, std::max<int64_t>(1, (kThreads + base - 1) / base)));
+  a.threads = base * a.chunks;
+  if ((a.threads + 255) / 256 >= kMaxBlocks) return fail(RT3D_ERR_UNSUPPORTED, "too many vectors for one call");
+  return launched(launch_rope(a, d->dtype, halves, pairs, stream));
+}
+
+rt3d_status rt3d_diffattn_fwd_workspace_size(const rt3d_diffattn_desc *d, uint64_t *bytes) {
+  Shape s;
+  const rt3d_status st = check_attn(d, false, s);
+  if (st != RT3D_OK) return st;
+  if (!bytes) return fail(RT3D_ERR_INVALID_ARG, "bytes must be non-NULL");
+  *bytes = fwd_plan(d, s, ~0ull).bytes;
+  return ok();
+}
+
+rt3d_status rt3d_diffattn_fwd(const rt3d_diffattn_desc *d, const void *q, const void *k, const void *v,
+                              const float *lambda, const int32_t *q_len, const int32_t *k_len, void *o, void *o2,
+                              float *lse, void *workspace, uint64_t workspace_bytes, void *stream) {
+  Shape s;
+  const rt3d_status st = check_attn(d, false, s);
+  if (st != RT3D_OK) return st;
+  if (d->n == 0 || d->lq == 0) return ok();
+  if (!q || !lambda || !o || (d->lk > 0 && (!k || !v)))
+    return fail(RT3D_ERR_INVALID_ARG, "q, k, v, lambda and o must be non-NULL");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(o2, 16) ||
+      !aligned(workspace, 16))
+    return fail(RT3D_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  if (!aligned(lambda, 4) || !aligned(lse, 4) || !aligned(q_len, 4) || !aligned(k_len, 4))
+    return fail(RT3D_ERR_INVALID_ARG, "lambda, lse and lengths must be 4-byte aligned");
+  const FwdPlan p = fwd_plan(d, s, workspace ? workspace_bytes : 0);
+  if (p.blocks >= kMaxBlocks) return fail(RT3D_ERR_UNSUPPORTED, "too many rows for one call");
+  AttnArgs a = attn_args(d, s);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.lam = lambda;
+  a.q_len = q_len;
+  a.k_len = k_len;
+  a.out = o;
+  a.out2 = o2;
+  a.lse = lse;
+  a.part = static_cast<float *>(workspace);
+  a.tiles = p.tiles;
+  a.splits = p.splits;
+  a.span = p.span;
+  a.blocks = p.blocks;
+  return launched(launch_attn_fwd(a, d->dtype, p.row_groups, stream));
+}
+
+rt3d_status rt3d_diffattn_bwd_workspace_size(const rt3d_diffattn_desc *d, uint64_t *bytes) {
+  Shape s;
+  const rt3d_status st = check_attn(d, true, s);
+  if (st != RT3D_OK) return st;
+  if (!bytes) return fail(RT3D_ERR_INVALID_ARG, "bytes must be non-NULL");
+  *bytes = bwd_workspace(d);
+  return ok();
+}
+
+rt3d_status rt3d_diffattn_bwd(const rt3d_diffattn_desc *d, const void *q, const void *k, const void *v,
+                              const float *lambda, const int32_t *q_len, const int32_t *k_len, const void *o,
+                              const void *o2, const float *lse, const void *d_o, void *dq, void *dk, void *dv,
+                              float *dlambda, void *workspace, uint64_t workspace_bytes, void *stream) {
+  Shape s;
+  const rt3d_status st = check_attn(d, true, s);
+  if (st != RT3D_OK) return st;
+  if (!dq && !dk && !dv && !dlambda) return ok();
+  const bool queries = d->n > 0 && d->lq > 0, keys = d->n > 0 && d->lk > 0;
+  if (queries && (!q || !lambda || !o || !o2 || !lse || !d_o))
+    return fail(RT3D_ERR_INVALID_ARG, "q, lambda, o, o2, lse and d_o must be non-NULL");
+  if (keys && (!k || !v)) return fail(RT3D_ERR_INVALID_ARG, "k and v must be non-NULL");
+  for (const void *p : {q, k, v, o, o2, d_o, static_cast<const void *>(dq), static_cast<const void *>(dk),
+                        static_cast<const void *>(dv), static_cast<const void *>(workspace)})
+    if (!aligned(p, 16)) return fail(RT3D_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+  if (!aligned(lambda, 4) || !aligned(lse, 4) || !aligned(dlambda, 4) || !aligned(q_len, 4) || !aligned(k_len, 4))
+    return fail(RT3D_ERR_INVALID_ARG, "lambda, dlambda, lse and lengths must be 4-byte aligned");
+  const uint64_t need = bwd_workspace(d);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(RT3D_ERR_BUFFER_TOO_SMALL, "the backward pass needs %llu bytes of workspace, got %llu",
+                static_cast<unsigned long long>(need),
+                static_cast<unsigned long long>(workspace ? workspace_bytes : 0));
+  AttnArgs a = attn_args(d, s);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.lam = lambda;
+  a.q_len = q_len;
+  a.k_len = k_len;
+  a.o = o;
+  a.o2 = o2;
+  a.lse = const_cast<float *>(lse);
+  a.d_o = d_o;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.dlam = dlambda;
+  a.rowstat = static_cast<float *>(workspace);
+  return launched(launch_attn_bwd(a, d->dtype, stream));
+}
+
+}  // extern "C"

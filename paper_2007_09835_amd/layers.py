@@ -95,3 +95,230 @@ def maxpool3d(x: torch.Tensor, k, stride, dtype: str, out: Optional[torch.Tensor
         out = torch.empty((n, to, ho, wo, c), dtype=x.dtype, device=x.device)
     rt3d.rt3d_maxpool3d_fwd(x, out, k, stride, dtype, stream, pad)
     return out
+
+
+# ---------------------------------------------------------------------------
+# Token operators
+#
+# Inputs are tensors whose last dimension is dense; views into wider rows (a
+# projection's queries beside its keys, the filled part of a cache) are taken as
+# they are.  Results are new tensors unless ``out`` is given.  A call runs on the
+# device of its tensors, on ``stream`` (a torch stream of that device) or else on
+# that device's current stream; its results and workspace belong to that stream.
+# ---------------------------------------------------------------------------
+
+_CODES = {dt: name for name, dt in TORCH_DTYPES.items()}
+
+
+def _dtype_of(x: torch.Tensor, name: str) -> str:
+    if x.dtype not in _CODES:
+        raise ValueError("%s must be float32, bfloat16 or float16, not %s" % (name, x.dtype))
+    return _CODES[x.dtype]
+
+
+def _need(t: Optional[torch.Tensor], name: str, like: torch.Tensor, shape, dtype) -> None:
+    """``t`` (if there is one) lies on ``like``'s device with this shape and type."""
+    if t is None:
+        return
+    if t.device != like.device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, like.device))
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, not %s" % (name, list(shape), list(t.shape)))
+
+
+def _launch(x: torch.Tensor, stream, call):
+    """``call()`` with ``x``'s device and ``stream`` current."""
+    if not x.is_cuda:
+        raise ValueError("tensors must be on a GPU")
+    if stream is not None:
+        if stream.device != x.device:
+            raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, x.device))
+        with torch.cuda.stream(stream):
+            return call()
+    if x.device.index != torch.cuda.current_device():
+        with torch.cuda.device(x.device):
+            return call()
+    return call()
+
+
+def _row_pitch(x: torch.Tensor, name: str) -> int:
+    """Elements between neighbouring rows (vectors along the last dimension)."""
+    c = x.shape[-1]
+    if x.is_contiguous():
+        return c
+    sizes = [(n, s) for n, s in zip(x.shape[:-1], x.stride()[:-1]) if n != 1]
+    pitch = sizes[-1][1] if sizes else c
+    for (_, outer), (n, inner) in zip(sizes, sizes[1:]):
+        if outer != n * inner:
+            raise ValueError("%s: its rows are not at one pitch" % name)
+    if pitch < c or (c > 1 and x.stride(-1) != 1):
+        raise ValueError("%s: its rows must be dense and apart" % name)
+    return pitch
+
+
+def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+               beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               out: Optional[torch.Tensor] = None, save: bool = False, stream=None):
+    """Layer norm of x [..., c] over its last dimension; gamma, beta: float32 [c].
+    With ``save`` also what ``layer_norm_backward`` needs."""
+    c = x.shape[-1]
+    dtype = _dtype_of(x, "x")
+    for t, name in ((gamma, "gamma"), (beta, "beta")):
+        _need(t, name, x, (c,), torch.float32)
+    _need(out, "out", x, x.shape, x.dtype)
+
+    def call():
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        rows = x.numel() // c if c else 0
+        mean = rstd = None
+        if save:
+            mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind()
+        d = rt3d.make_norm_desc(rows, c, dtype, eps, _row_pitch(x, "x"), _row_pitch(y, "out"))
+        rt3d.rt3d_layernorm_fwd(d, x, gamma, beta, y, mean, rstd)
+        return (y, (mean, rstd)) if save else y
+
+    return _launch(x, stream, call)
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], saved,
+                        stream=None):
+    """(dx, dgamma, dbeta) of ``layer_norm(x, gamma, ..., save=True)``; dx has x's
+    layout."""
+    c = x.shape[-1]
+    dtype = _dtype_of(x, "x")
+    rows = x.numel() // c if c else 0
+    mean, rstd = saved
+    _need(dy, "dy", x, x.shape, x.dtype)
+    _need(gamma, "gamma", x, (c,), torch.float32)
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _need(t, name, x, (rows,), torch.float32)
+
+    def call():
+        d = rt3d.make_norm_desc(rows, c, dtype, 1.0, _row_pitch(x, "x"), _row_pitch(dy, "dy"))
+        dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+        dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=x.device).unbind()
+        ws = torch.empty(rt3d.rt3d_layernorm_bwd_workspace_size(d) // 4, dtype=torch.float32,
+                         device=x.device)
+        rt3d.rt3d_layernorm_bwd(d, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws)
+        return dx, dgamma, dbeta
+
+    return _launch(x, stream, call)
+
+
+def _rows_of(x: torch.Tensor, width: int, name: str):
+    """(pitch, batch) of a [n, tokens, ...] tensor whose tokens hold ``width``
+    dense elements."""
+    inner = 1
+    for size, step in zip(reversed(x.shape[2:]), reversed(x.stride()[2:])):
+        if size != 1 and step != inner:
+            raise ValueError("%s: a token's vectors must be dense" % name)
+        inner *= size
+    pitch = x.stride(1) if x.shape[1] > 1 else width
+    if pitch < width or (x.shape[0] > 1 and x.stride(0) <= 0 and x.numel()):
+        raise ValueError("%s: its tokens or clips share memory" % name)
+    return pitch, x.stride(0) if x.shape[0] > 1 else 0
+
+
+def rope3d(x: torch.Tensor, grid: Sequence[int], sections: Sequence[int], base: float = 10000.0,
+           t0: int = 0, pos: Optional[torch.Tensor] = None, halves: bool = False,
+           inverse: bool = False, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rotates the vectors of x [n, tokens, vecs, d] by their token's place in the
+    (t, h, w) ``grid``, or by ``pos`` (int32 [n, tokens, 3]).  ``sections``: the
+    channels that turn with time, row and column.  ``inverse`` turns back: the
+    backward pass.  ``out`` may be x."""
+    n, tokens, vecs, d = x.shape
+    dtype = _dtype_of(x, "x")
+    if len(grid) != 3 or len(sections) != 3:
+        raise ValueError("grid and sections have three axes")
+    if grid[0] * grid[1] * grid[2] != tokens:
+        raise ValueError("a %s grid has not %d tokens" % (tuple(grid), tokens))
+    _need(out, "out", x, x.shape, x.dtype)
+    _need(pos, "pos", x, (n, tokens, 3), torch.int32)
+
+    def call():
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        desc = rt3d.make_rope_desc(n, grid, vecs, d, sections, dtype, base, t0, halves, inverse,
+                                   _rows_of(x, vecs * d, "x"), _rows_of(y, vecs * d, "out"))
+        rt3d.rt3d_rope3d(desc, x, pos, y)
+        return y
+
+    return _launch(x, stream, call)
+
+
+def _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, **more):
+    """Checks the inputs of differential attention and fills their descriptor."""
+    if q.dim() != 5 or q.shape[3] != 2:
+        raise ValueError("q must be [n, lq, hq, 2, d], not %s" % list(q.shape))
+    n, lq, hq, _, d = q.shape
+    if k.dim() != 5:
+        raise ValueError("k must be [n, lk, hk, 2, d], not %s" % list(k.shape))
+    lk, hk = k.shape[1:3]
+    _need(k, "k", q, (n, lk, hk, 2, d), q.dtype)
+    _need(v, "v", q, (n, lk, hk, 2 * d), q.dtype)
+    _need(lam, "lam", q, (hq,), torch.float32)
+    _need(q_len, "q_len", q, (n,), torch.int32)
+    _need(k_len, "k_len", q, (n,), torch.int32)
+    rows = {"q": _rows_of(q, hq * 2 * d, "q"), "k": _rows_of(k, hk * 2 * d, "k"),
+            "v": _rows_of(v, hk * 2 * d, "v")}
+    for name, t in more.items():
+        if t is not None:
+            rows[name] = _rows_of(t, t.shape[2] * 2 * d, name)
+    return rt3d.make_diffattn_desc(n, lq, lk, hq, hk, d, _dtype_of(q, "q"), frame,
+                                   0.0 if scale is None else scale, **rows)
+
+
+def diff_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor,
+                   frame: int = 0, q_len: Optional[torch.Tensor] = None,
+                   k_len: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                   out: Optional[torch.Tensor] = None, save: bool = False, stream=None):
+    """Differential attention: q [n, lq, hq, 2, d], k [n, lk, hk, 2, d], v [n, lk,
+    hk, 2 d], lam float32 [hq] -> [n, lq, hq, 2 d].  ``frame`` tokens make a frame of
+    the causal mask (0: none); ``q_len``, ``k_len`` (int32 [n]): the clips' lengths in
+    a padded batch or a cache.  With ``save`` also what
+    ``diff_attention_backward`` needs."""
+    desc = _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=out)
+    n, lq, hq, _, d = q.shape
+    shape = (n, lq, hq, 2 * d)
+    _need(out, "out", q, shape, q.dtype)
+
+    def call():
+        o = torch.empty(shape, dtype=q.dtype, device=q.device) if out is None else out
+        o2 = lse = ws = None
+        if save:
+            o2 = torch.empty(shape, dtype=q.dtype, device=q.device)
+            lse = torch.empty((2, n, hq, lq), dtype=torch.float32, device=q.device)
+        nbytes = rt3d.rt3d_diffattn_fwd_workspace_size(desc)
+        if nbytes:
+            ws = torch.empty(nbytes // 4, dtype=torch.float32, device=q.device)
+        rt3d.rt3d_diffattn_fwd(desc, q, k, v, lam, q_len, k_len, o, o2, lse, ws)
+        return (o, (o, o2, lse)) if save else o
+
+    return _launch(q, stream, call)
+
+
+def diff_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                            lam: torch.Tensor, saved, frame: int = 0,
+                            q_len: Optional[torch.Tensor] = None,
+                            k_len: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                            stream=None):
+    """(dq, dk, dv, dlam) of ``diff_attention(..., save=True)`` with the same
+    arguments."""
+    o, o2, lse = saved
+    n, lq, hq, _, d = q.shape
+    _need(do, "do", q, (n, lq, hq, 2 * d), q.dtype)
+    _need(o, "o", q, do.shape, q.dtype)
+    _need(o2, "o2", q, do.shape, q.dtype)
+    _need(lse, "lse", q, (2, n, hq, lq), torch.float32)
+    desc = _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=o, d_o=do)
+
+    def call():
+        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dlam = torch.empty(hq, dtype=torch.float32, device=q.device)
+        nbytes = rt3d.rt3d_diffattn_bwd_workspace_size(desc)
+        ws = torch.empty(nbytes // 4, dtype=torch.float32, device=q.device) if nbytes else None
+        rt3d.rt3d_diffattn_bwd(desc, q, k, v, lam, q_len, k_len, o, o2, lse, do, dq, dk, dv, dlam, ws)
+        return dq, dk, dv, dlam
+
+    return _launch(q, stream, call)

@@ -39,10 +39,16 @@ EXPORTED = (
     "rt3d_kgs_pack_size", "rt3d_kgs_pack", "rt3d_kgs_unpack", "rt3d_conv3d_workspace_size",
     "rt3d_conv3d_launch_info", "rt3d_kgs_conv3d_fwd", "rt3d_kgs_conv3d_fwd_noalloc", "rt3d_dense_pack_size", "rt3d_dense_pack", "rt3d_conv3d_dense_fwd",
     "rt3d_maxpool3d_fwd", "rt3d_group_units", "rt3d_group_workspace_size", "rt3d_group_reweight",
+    "rt3d_layernorm_fwd", "rt3d_layernorm_bwd_workspace_size", "rt3d_layernorm_bwd", "rt3d_rope3d",
+    "rt3d_diffattn_fwd_workspace_size", "rt3d_diffattn_fwd", "rt3d_diffattn_bwd_workspace_size",
+    "rt3d_diffattn_bwd",
 )
 
 RT3D_SCOPE_KGS = 0
 RT3D_SCOPE_VANILLA = 1
+
+RT3D_ROPE_HALVES = 1
+RT3D_ROPE_INVERSE = 2
 
 
 class Rt3dError(RuntimeError):
@@ -87,6 +93,28 @@ class GroupDesc(ctypes.Structure):
         "c_out", "c_in", "kt", "kh", "kw", "g_m", "g_n", "dtype", "norm", "scope")]
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("x_pitch", ctypes.c_int64), ("y_pitch", ctypes.c_int64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("pitch", ctypes.c_int64), ("batch", ctypes.c_int64)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in (
+        "n", "t", "h", "w", "vecs", "d", "dt", "dh", "dw", "t0")] + [
+        ("base", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("x", Rows), ("y", Rows)]
+
+
+class DiffAttnDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in (
+        "n", "lq", "lk", "hq", "hk", "d", "dtype", "frame")] + [("scale", ctypes.c_float)] + [
+        (name, Rows) for name in ("q", "o", "k", "v", "d_o", "dq", "dk", "dv")]
+
+
 _lib = None
 
 
@@ -123,6 +151,14 @@ def load():
         "rt3d_group_workspace_size": ([P(GroupDesc), P(u64)], ctypes.c_int),
         "rt3d_group_reweight": ([P(GroupDesc), vp, vp] + [ctypes.c_float] * 4 + [vp] * 7 +
                                 [u64, vp], ctypes.c_int),
+        "rt3d_layernorm_fwd": ([P(NormDesc)] + [vp] * 7, ctypes.c_int),
+        "rt3d_layernorm_bwd_workspace_size": ([P(NormDesc), P(u64)], ctypes.c_int),
+        "rt3d_layernorm_bwd": ([P(NormDesc)] + [vp] * 9 + [u64, vp], ctypes.c_int),
+        "rt3d_rope3d": ([P(RopeDesc), vp, vp, vp, vp], ctypes.c_int),
+        "rt3d_diffattn_fwd_workspace_size": ([P(DiffAttnDesc), P(u64)], ctypes.c_int),
+        "rt3d_diffattn_fwd": ([P(DiffAttnDesc)] + [vp] * 10 + [u64, vp], ctypes.c_int),
+        "rt3d_diffattn_bwd_workspace_size": ([P(DiffAttnDesc), P(u64)], ctypes.c_int),
+        "rt3d_diffattn_bwd": ([P(DiffAttnDesc)] + [vp] * 15 + [u64, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -335,3 +371,98 @@ def rt3d_group_reweight(desc: GroupDesc, w, pen=None, lam=1.0, eps=1e-6, tau=0.0
         _dev_ptr(reg, "reg"), _dev_ptr(mask, "mask"), _dev_ptr(grad, "grad"),
         _dev_ptr(w_prox, "w_prox"), _dev_ptr(workspace, "workspace"), ws_bytes,
         _stream_ptr(stream)))
+
+
+# Token operators.  Tensors may be strided views whose last dimension is dense;
+# the descriptor holds their pitches.
+
+def _view_ptr(t, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.numel() and t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError("%s must be dense along its last dimension" % name)
+    return t.data_ptr()
+
+
+def _ws(workspace):
+    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dev_ptr(workspace, "workspace"), n
+
+
+def _size(fn, desc) -> int:
+    out = ctypes.c_uint64()
+    _check(fn(ctypes.byref(desc), ctypes.byref(out)))
+    return out.value
+
+
+def make_norm_desc(rows, c, dtype="bf16", eps=1e-5, x_pitch=0, y_pitch=0) -> NormDesc:
+    """Fill an rt3d_norm_desc."""
+    return NormDesc(rows, c, DTYPE_CODES[dtype], eps, x_pitch, y_pitch)
+
+
+def rt3d_layernorm_fwd(desc: NormDesc, x, gamma, beta, y, mean=None, rstd=None, stream=None) -> None:
+    _check(load().rt3d_layernorm_fwd(
+        ctypes.byref(desc), _view_ptr(x, "x"), _dev_ptr(gamma, "gamma"), _dev_ptr(beta, "beta"),
+        _view_ptr(y, "y"), _dev_ptr(mean, "mean"), _dev_ptr(rstd, "rstd"), _stream_ptr(stream)))
+
+
+def rt3d_layernorm_bwd_workspace_size(desc: NormDesc) -> int:
+    return _size(load().rt3d_layernorm_bwd_workspace_size, desc)
+
+
+def rt3d_layernorm_bwd(desc: NormDesc, x, dy, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None,
+                       workspace=None, stream=None) -> None:
+    _check(load().rt3d_layernorm_bwd(
+        ctypes.byref(desc), _view_ptr(x, "x"), _view_ptr(dy, "dy"), _dev_ptr(gamma, "gamma"),
+        _dev_ptr(mean, "mean"), _dev_ptr(rstd, "rstd"), _view_ptr(dx, "dx"),
+        _dev_ptr(dgamma, "dgamma"), _dev_ptr(dbeta, "dbeta"), *_ws(workspace), _stream_ptr(stream)))
+
+
+def make_rope_desc(n, grid, vecs, d, sections, dtype="bf16", base=10000.0, t0=0, halves=False,
+                   inverse=False, x=(0, 0), y=(0, 0)) -> RopeDesc:
+    """Fill an rt3d_rope_desc (``x``, ``y``: (pitch, batch) of their rows)."""
+    flags = (RT3D_ROPE_HALVES if halves else 0) | (RT3D_ROPE_INVERSE if inverse else 0)
+    return RopeDesc(n, *grid, vecs, d, *sections, t0, base, DTYPE_CODES[dtype], flags, Rows(*x),
+                    Rows(*y))
+
+
+def rt3d_rope3d(desc: RopeDesc, x, pos, y, stream=None) -> None:
+    _check(load().rt3d_rope3d(ctypes.byref(desc), _view_ptr(x, "x"), _dev_ptr(pos, "pos"),
+                              _view_ptr(y, "y"), _stream_ptr(stream)))
+
+
+def make_diffattn_desc(n, lq, lk, hq, hk, d, dtype="bf16", frame=0, scale=0.0, **rows) -> DiffAttnDesc:
+    """Fill an rt3d_diffattn_desc; ``rows``: (pitch, batch) by tensor (q, o, k,
+    v, d_o, dq, dk, dv), tight where absent."""
+    return DiffAttnDesc(n, lq, lk, hq, hk, d, DTYPE_CODES[dtype], frame, scale,
+                        *(Rows(*rows.get(name, (0, 0)))
+                          for name in ("q", "o", "k", "v", "d_o", "dq", "dk", "dv")))
+
+
+def rt3d_diffattn_fwd_workspace_size(desc: DiffAttnDesc) -> int:
+    return _size(load().rt3d_diffattn_fwd_workspace_size, desc)
+
+
+def rt3d_diffattn_fwd(desc: DiffAttnDesc, q, k, v, lam, q_len, k_len, o, o2=None, lse=None,
+                      workspace=None, stream=None) -> None:
+    _check(load().rt3d_diffattn_fwd(
+        ctypes.byref(desc), _view_ptr(q, "q"), _view_ptr(k, "k"), _view_ptr(v, "v"),
+        _dev_ptr(lam, "lambda"), _dev_ptr(q_len, "q_len"), _dev_ptr(k_len, "k_len"),
+        _view_ptr(o, "o"), _dev_ptr(o2, "o2"), _dev_ptr(lse, "lse"), *_ws(workspace),
+        _stream_ptr(stream)))
+
+
+def rt3d_diffattn_bwd_workspace_size(desc: DiffAttnDesc) -> int:
+    return _size(load().rt3d_diffattn_bwd_workspace_size, desc)
+
+
+def rt3d_diffattn_bwd(desc: DiffAttnDesc, q, k, v, lam, q_len, k_len, o, o2, lse, d_o, dq=None,
+                      dk=None, dv=None, dlam=None, workspace=None, stream=None) -> None:
+    _check(load().rt3d_diffattn_bwd(
+        ctypes.byref(desc), _view_ptr(q, "q"), _view_ptr(k, "k"), _view_ptr(v, "v"),
+        _dev_ptr(lam, "lambda"), _dev_ptr(q_len, "q_len"), _dev_ptr(k_len, "k_len"),
+        _view_ptr(o, "o"), _dev_ptr(o2, "o2"), _dev_ptr(lse, "lse"), _view_ptr(d_o, "d_o"),
+        _view_ptr(dq, "dq"), _view_ptr(dk, "dk"), _view_ptr(dv, "dv"), _dev_ptr(dlam, "dlambda"),
+        *_ws(workspace), _stream_ptr(stream)))

@@ -1,0 +1,232 @@
+"""Differential attention on the GPU, forward, backward and for single tokens,
+against the 64-bit reference, within the bounds that token_refs derives."""
+import pytest
+import torch
+
+import token_refs as refs
+from paper_2007_09835_amd import build, layers
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    build.build(force=False)
+
+
+def _inputs(seed, n, lq, lk, hq, hk, d, dtype, spread=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=gen)
+    q = refs.rounded(r(n, lq, hq, 2, d) * spread, dtype)
+    k = refs.rounded(r(n, lk, hk, 2, d), dtype)
+    v = refs.rounded(r(n, lk, hk, 2 * d) + 0.3, dtype)
+    do = refs.rounded(r(n, lq, hq, 2 * d), dtype)
+    lam = r(hq) * 0.2 + 0.6
+    return q, k, v, do, lam
+
+
+def _check(seed, n, lq, lk, hq, hk, d, dtype, frame=0, q_len=None, k_len=None, scale=None, spread=1.0):
+    q, k, v, do, lam = _inputs(seed, n, lq, lk, hq, hk, d, dtype, spread)
+    dev = lambda t: None if t is None else torch.tensor(t, dtype=torch.int32).cuda()
+    more = dict(frame=frame, q_len=dev(q_len), k_len=dev(k_len), scale=scale)
+    args = (q[0].cuda(), k[0].cuda(), v[0].cuda(), lam.cuda())
+    only = layers.diff_attention(*args, **more)
+    o, saved = layers.diff_attention(*args, save=True, **more)
+    grads = layers.diff_attention_backward(do[0].cuda(), *args, saved, **more)
+    torch.cuda.synchronize()
+    assert torch.equal(only, o)
+    h = 0.0 if dtype == "f32" else refs.HALF[dtype]
+    ref = refs.diff_attention(q[1], k[1], v[1], lam.double(), frame, q_len, k_len, scale, do[1], h,
+                              refs.TINY[dtype])
+    tiny = refs.TINY[dtype] * 4 + 1e-30
+    half = refs.U if dtype == "f32" else 0.0  # the f32 result's own rounding
+    refs.within(o, ref["o"], ref["o_err"] + half * ref["o"].abs() + tiny, "o")
+    for name, got in zip(("dq", "dk", "dv", "dlam"), grads):
+        refs.within(got, ref[name], ref[name + "_err"] + half * ref[name].abs() + tiny, name)
+    seen = torch.isfinite(ref["lse"])
+    lse = saved[2].double().cpu()
+    assert torch.equal(torch.isfinite(lse), seen)
+    assert ((lse - ref["lse"])[seen].abs() <= 1e-4).all()
+    return o, grads, ref
+
+
+SHAPES = [
+    # n, lq, lk, hq, hk, d
+    (1, 1, 1, 1, 1, 8), (2, 1, 33, 2, 1, 16), (1, 7, 3, 2, 2, 32), (2, 33, 65, 4, 2, 32),
+    (1, 98, 98, 8, 8, 32), (2, 130, 70, 4, 1, 64), (1, 64, 129, 2, 2, 40), (1, 100, 200, 2, 1, 128),
+    (1, 31, 66, 3, 1, 72), (1, 200, 31, 1, 1, 24),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("frame", [0, 1, 13])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_forward_and_backward(shape, frame, dtype):
+    _check(11, *shape, dtype, frame)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("frame", [0, 1, 5])
+@pytest.mark.parametrize("q_len,k_len", [([70, 1, 0, 33], [70, 70, 40, 64]), ([70, 64, 10, 31], [1, 0, 32, 31])])
+def test_padded_batches(q_len, k_len, frame, dtype):
+    o, (dq, dk, dv, _), _ = _check(5, 4, 70, 70, 4, 2, 32, dtype, frame, q_len, k_len)
+    for b in range(4):
+        assert not o[b, q_len[b]:].any() and not dq[b, q_len[b]:].any()
+        assert not dk[b, k_len[b]:].any() and not dv[b, k_len[b]:].any()
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_padding_is_never_read(d):
+    """NaN and infinities behind the lengths, in a cache's spare places, between rows
+    and between clips change nothing."""
+    n, lq, lk, hq, hk = 2, 50, 90, 4, 2
+    q, k, v, do, lam = _inputs(3, n, lq, lk, hq, hk, d, "bf16")
+    q_len, k_len = torch.tensor([50, 20], dtype=torch.int32).cuda(), torch.tensor([61, 90], dtype=torch.int32).cuda()
+
+    def spread(t, lens, poison):
+        tokens, width = t.shape[1], t[0, 0].numel()
+        big = torch.full((n, tokens + 5, width + 24), poison, dtype=t.dtype)
+        for b in range(n):
+            big[b, :int(lens[b]), :width] = t[b, :int(lens[b])].reshape(-1, width)
+        return big.cuda()[:, :tokens, :width].view(t.shape)
+
+    got = []
+    for poison in (0.0, float("nan"), float("inf")):
+        args = [spread(t[0], l, poison) for t, l in ((q, q_len), (k, k_len), (v, k_len))] + [lam.cuda()]
+        g = spread(do[0], q_len, poison)
+        o, saved = layers.diff_attention(*args, q_len=q_len, k_len=k_len, frame=7, save=True)
+        got.append((o, *layers.diff_attention_backward(g, *args, saved, q_len=q_len, k_len=k_len, frame=7)))
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 32), ("f32", 64), ("bf16", 128), ("f32", 96)])
+@pytest.mark.parametrize("lq,frame", [(1, 0), (1, 1), (3, 1), (16, 0), (40, 4)])
+def test_few_queries_against_a_cache(lq, frame, dtype, d):
+    """Splits of the keys, one of them behind the shortest clip; the workspace may be
+    absent, and the results agree within two roundings of the type."""
+    from paper_2007_09835_amd import rt3d
+    n, lk, hq, hk = 3, 2100, 4, 1
+    k_len = [2100, 300, 1]
+    o, _, _ = _check(17, n, lq, lk, hq, hk, d, dtype, frame, None, k_len, spread=1.5)
+    desc = rt3d.make_diffattn_desc(n, lq, lk, hq, hk, d, dtype, frame)
+    assert rt3d.rt3d_diffattn_fwd_workspace_size(desc) > 0
+    q, k, v, _, lam = _inputs(17, n, lq, lk, hq, hk, d, dtype, 1.5)
+    whole = torch.empty_like(o)
+    rt3d.rt3d_diffattn_fwd(desc, q[0].cuda(), k[0].cuda(), v[0].cuda(), lam.cuda(), None,
+                           torch.tensor(k_len, dtype=torch.int32).cuda(), whole)
+    ref = refs.diff_attention(q[1], k[1], v[1], lam.double(), frame, None, k_len,
+                              h=0.0 if dtype == "f32" else refs.HALF[dtype], tiny=refs.TINY[dtype])
+    half = refs.U if dtype == "f32" else 0.0
+    refs.within(whole, ref["o"], ref["o_err"] + half * ref["o"].abs() + refs.TINY[dtype] * 4 + 1e-30, "unsplit")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_sharp_and_flat_scores(dtype):
+    """Scores over a wide range (one key takes nearly all), and all equal."""
+    _check(23, 1, 40, 300, 2, 1, 32, dtype, spread=12.0)
+    _check(24, 1, 40, 300, 2, 1, 32, dtype, spread=0.0)
+    _check(25, 1, 40, 300, 2, 1, 32, dtype, scale=0.9)
+
+
+def test_scores_that_rise_along_the_keys():
+    """Every tile raises the running maximum of one map and not of the other."""
+    n, lk, d = 1, 700, 32
+    q, k, v, _, lam = _inputs(31, n, 33, lk, 1, 1, d, "bf16", 0.3)
+    ramp = torch.linspace(0, 40, lk)
+    for m, r in ((0, ramp), (1, -ramp)):
+        for which in (0, 1):
+            kk = k[which]
+            kk[0, :, 0, m, 0] = r.to(kk.dtype)
+            qq = q[which]
+            qq[0, :, 0, m, 0] = 8.0
+    k1 = k[0].double()
+    o = layers.diff_attention(q[0].cuda(), k[0].cuda(), v[0].cuda(), lam.cuda())
+    ref = refs.diff_attention(q[0].double(), k1, v[1], lam.double(), h=refs.HALF["bf16"])
+    refs.within(o, ref["o"], ref["o_err"], "o")
+
+
+def test_repeated_calls_and_other_streams():
+    q, k, v, do, lam = _inputs(7, 2, 150, 150, 4, 2, 64, "bf16")
+    args = [t[0].cuda() for t in (q, k, v)] + [lam.cuda()]
+    g = do[0].cuda()
+
+    def run(stream=None):
+        o, saved = layers.diff_attention(*args, frame=10, save=True, stream=stream)
+        return (o, *layers.diff_attention_backward(g, *args, saved, frame=10, stream=stream))
+
+    first = run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for s in (None, side, None, side):
+        again = run(s)
+        torch.cuda.synchronize()
+        for a, b in zip(first, again):
+            assert torch.equal(a, b)
+
+
+def test_offsets_past_32_bits():
+    """A cache whose last clip begins beyond 2^32 bytes."""
+    n, cap, hk, d = 3, 530000, 8, 128
+    k = torch.zeros(n, cap, hk, 2, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros(n, cap, hk, 2 * d, dtype=torch.bfloat16, device="cuda")
+    q, kk, vv, _, lam = _inputs(2, n, 1, 64, 8, hk, d, "bf16")
+    lens = torch.tensor([cap, 10, cap], dtype=torch.int32).cuda()
+    # the last 64 places of long clips and the first of the short one
+    k[0, -64:], v[0, -64:] = kk[0][0].cuda(), vv[0][0].cuda()
+    k[2, -64:], v[2, -64:] = kk[0][2].cuda(), vv[0][2].cuda()
+    k[1, :64], v[1, :64] = kk[0][1].cuda(), vv[0][1].cuda()
+    o = layers.diff_attention(q[0].cuda(), k, v, lam.cuda(), k_len=lens, scale=1.0)
+    torch.cuda.synchronize()
+    h = refs.HALF["bf16"]
+    for b in range(n):
+        # zero keys score 0 with value 0: they only add to the denominators
+        zeros = cap - 64 if b != 1 else 0
+        m = 64 if b != 1 else 10
+        for head in range(8):
+            ps = []
+            for i in range(2):
+                e = torch.exp(kk[1][b, :m, head, i] @ q[1][b, 0, head, i])
+                ps.append(e / (e.sum() + zeros))
+            ref = (ps[0] - lam[head].double() * ps[1]) @ vv[1][b, :m, head]
+            size = (ps[0] + lam[head].double() * ps[1]) @ vv[1][b, :m, head].abs()
+            # scores of up to 60 in 32 bits: (d + 8) u |s| < 5e-4; roundings as above
+            err = (2 * h + 2e-3) * size + h * ref.abs()
+            refs.within(o[b, 0, head], ref, err, f"clip {b}")
+
+
+def test_gradients_against_differences_of_the_forward_kernel():
+    """f32, central differences with a step of 1e-2: the third derivative and the
+    rounding of two losses leave less than 3e-3 of the largest gradient."""
+    q, k, v, do, lam = _inputs(41, 1, 5, 6, 2, 1, 8, "f32")
+    args = [t[0].cuda() for t in (q, k, v)] + [lam.cuda()]
+    g = do[0].cuda()
+    _, saved = layers.diff_attention(*args, frame=2, save=True)
+    grads = layers.diff_attention_backward(g, *args, saved, frame=2)
+    loss = lambda: (layers.diff_attention(*args, frame=2).double() * g.double()).sum().item()
+    for grad, of in zip(grads, args):
+        flat = of.view(-1)
+        for i in range(0, flat.numel(), max(1, flat.numel() // 12)):
+            keep = flat[i].item()
+            flat[i] = keep + 1e-2
+            hi, up = loss(), flat[i].item()
+            flat[i] = keep - 1e-2
+            lo, down = loss(), flat[i].item()
+            flat[i] = keep
+            assert abs((hi - lo) / (up - down) - grad.view(-1)[i].item()) <= 3e-3 * max(1.0, grad.abs().max().item())
+
+
+def test_nothing_to_do():
+    lam = torch.ones(2, device="cuda")
+    e = lambda *s: torch.empty(s, device="cuda", dtype=torch.bfloat16)
+    o = layers.diff_attention(e(0, 3, 2, 2, 16), e(0, 3, 2, 2, 16), e(0, 3, 2, 32), lam)
+    assert o.shape == (0, 3, 2, 32)
+    q, k, v = e(2, 3, 2, 2, 16).zero_(), e(2, 0, 2, 2, 16), e(2, 0, 2, 32)
+    o, saved = layers.diff_attention(q, k, v, lam, save=True)
+    dq, dk, dv, dl = layers.diff_attention_backward(torch.ones_like(o), q, k, v, lam, saved)
+    assert not o.any() and not dq.any() and dk.numel() == 0 and not dl.any()
+    q, k, v = e(2, 0, 2, 2, 16), e(2, 3, 2, 2, 16).zero_(), e(2, 3, 2, 32).zero_()
+    o, saved = layers.diff_attention(q, k, v, lam, save=True)
+    dq, dk, dv, dl = layers.diff_attention_backward(o, q, k, v, lam, saved)
+    assert not dk.any() and not dv.any() and not dl.any()
