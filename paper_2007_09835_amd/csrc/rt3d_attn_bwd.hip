@@ -186,11 +186,14 @@ struct Dkv {
   static constexpr int kThreads = 64 * WAVES;
   using Q = Tile<T, D, kRows, kThreads>;
   static constexpr int kStat = 4 * 64 * 4;  // logarithms and row sums of the tile's rows
-  static constexpr int kLds = 2 * (2 * Q::kBytes + kStat);
   static constexpr int kMinWaves = sizeof(T) == 2 && D <= 64 ? 2 : 1;
-  // 32-bit keys and values of 128 and 256 columns beside their gradients pass the
-  // register file: they are read again for every tile (from L1).
-  static constexpr bool kHold = sizeof(T) == 2 || D <= 64;
+  // Values stay in registers, and keys where both fit beside their gradients;
+  // otherwise keys wait in LDS.  32-bit values of 256 columns (and their keys)
+  // pass both: they are read again for every tile, from L1.
+  static constexpr bool kHoldV = sizeof(T) == 2 || D <= 64, kHoldK = D <= 32, kLdsK = !kHoldK && kHoldV;
+  using K = Tile<T, D, 32 * WAVES, kThreads>;
+  static constexpr int kBuffer = 2 * Q::kBytes + kStat;
+  static constexpr int kLds = 2 * kBuffer + (kLdsK ? K::kBytes : 0);
 };
 
 template <typename T, int D, int WAVES>
@@ -234,12 +237,22 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       const int col = s * 16 + 8 * half;
       return in && col < 2 * a.d ? load_frag(v + col) : Frag<T>{};
     };
-    Frag<T> kf[F::kHold ? 2 : 1][F::kHold ? D / 16 : 1], vf[F::kHold ? 2 * D / 16 : 1];
-    if constexpr (F::kHold) {
+    Frag<T> kf[F::kHoldK ? 2 : 1][F::kHoldK ? D / 16 : 1], vf[F::kHoldV ? 2 * D / 16 : 1];
+    if constexpr (F::kHoldK) {
 #pragma unroll
       for (int s = 0; s < D / 16; ++s) kf[0][s] = key_frag(0, s), kf[1][s] = key_frag(1, s);
+    }
+    if constexpr (F::kHoldV) {
 #pragma unroll
       for (int s = 0; s < 2 * D / 16; ++s) vf[s] = value_frag(s);
+    }
+    lds_char *keys = lds + 2 * F::kBuffer;
+    if constexpr (F::kLdsK) {
+      unsigned k_off[F::K::kLoads];
+      F::K::template offsets<true>(a.d, a.k_pitch, k_off);
+      F::K::stage(static_cast<const T *>(a.k) + clip * a.k_batch + key_block * a.k_pitch +
+                      static_cast<int64_t>(kvh) * 2 * a.d,
+                  min(32 * WAVES, k_len - key_block), a.d, a.k_pitch, k_off, keys);
     }
     unsigned q_off[Q::kLoads], g_off[Q::kLoads];
     Q::template offsets<true>(a.d, a.q_pitch, q_off);
@@ -252,7 +265,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
     int st_head = 0, st_row = begin;  // of the tile to be staged next
     auto stage = [&](int buf) {
       const int head = kvh * a.group + st_head, n = min(kRows, q_len - st_row);
-      lds_char *to = lds + buf * (2 * Q::kBytes + F::kStat);
+      lds_char *to = lds + buf * F::kBuffer;
       Q::stage(q + st_row * a.q_pitch + static_cast<int64_t>(head) * 2 * a.d, n, a.d, a.q_pitch, q_off, to);
       Q::stage(go + st_row * a.do_pitch + static_cast<int64_t>(head) * 2 * a.d, n, a.d, a.do_pitch, g_off,
                to + Q::kBytes);
@@ -285,7 +298,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       }
       // no row of the tile sees a key of this wave, or it has none
       if (at + kRows <= from_wave || key_wave >= k_len) continue;
-      const lds_char *qt = lds + buf * (2 * Q::kBytes + F::kStat), *gt = qt + Q::kBytes, *st = gt + Q::kBytes;
+      const lds_char *qt = lds + buf * F::kBuffer, *gt = qt + Q::kBytes, *st = gt + Q::kBytes;
       // some pair of the tile is masked, or some row has a single key
       const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
       const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
@@ -293,21 +306,23 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
 #pragma unroll
       for (int i = 0; i < 2 * D / 16; ++i) {
         Frag<T> b;
-        if constexpr (F::kHold) b = vf[i];
+        if constexpr (F::kHoldV) b = vf[i];
         else b = value_frag(i);
         dp = Mma<T>::run(Q::along(gt, 0, i * 16), b, dp);
       }
-      Frag<T> ds[2][2];
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         f32x16 s = {};
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
           Frag<T> b;
-          if constexpr (F::kHold) b = kf[m][i];
+          if constexpr (F::kHoldK) b = kf[m][i];
+          else if constexpr (F::kLdsK) b = F::K::along(keys, wave * 32, m * D + i * 16);
           else b = key_frag(m, i);
           s = Mma<T>::run(Q::along(qt, 0, m * D + i * 16), b, s);
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -333,19 +348,20 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
           for (int i = 0; i < 16; ++i)
             if (single_all || at + result_row(i, half) == single) s[i] = 0.f;
         }
-        ds[m][0] = pack<T>(s, 0);
-        ds[m][1] = pack<T>(s, 8);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const Frag<T> ds = pack<T>(s, 8 * h);
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c)
+            dk[m][c] = Mma<T>::run(Q::across(qt, 16 * h, m * D + c * 32), ds, dk[m][c]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const Frag<T> p = pack<T>(pv, 8 * h);
 #pragma unroll
         for (int c = 0; c < 2 * D / 32; ++c) dv[c] = Mma<T>::run(Q::across(gt, 16 * h, c * 32), p, dv[c]);
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c)
-            dk[m][c] = Mma<T>::run(Q::across(qt, 16 * h, m * D + c * 32), ds[m][h], dk[m][c]);
       }
     }
   }
