@@ -250,50 +250,86 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
   }
 }
 
-// Joins the splits of a call with few rows, in their order: one wave per row.
+// Joins the splits of a row in their order.  A workgroup per row: the splits'
+// weights first (one thread each), then a thread per map and column.
+constexpr int kMaxSplits = 256;
 template <typename T>
-__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a) {
-  const int rows = a.lq * a.group;
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  __shared__ float weight[2][kMaxSplits], second[256];
+  const int rows = a.lq * a.group, tid = threadIdx.x;
   const int64_t r = blockIdx.x, total = static_cast<int64_t>(a.n) * a.hk * rows;
   const int row = static_cast<int>(r % rows);
   const int64_t pair = r / rows;
   const int kvh = static_cast<int>(pair % a.hk), clip = static_cast<int>(pair / a.hk);
   const int query = row / a.group, head = kvh * a.group + (row - query * a.group);
   const bool in = query < clip_length(a.q_len, clip, a.lq);
-  const float *st = a.part + r * 4;
-  float top[2] = {-INFINITY, -INFINITY};
-  for (int s = 0; in && s < a.splits; ++s)
+  // a wave's lanes take splits lane, lane + 64, ...: four at most
+  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+  if (in && tid < 64) {
+    f32x4 st[kMaxSplits / 64];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], st[s * total * 4 + 2 * m]);
-  const bool any = top[0] > -INFINITY;
-  float sum[2] = {0.f, 0.f};
-  for (int s = 0; any && s < a.splits; ++s)
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+      const int s = i * 64 + tid;
+      st[i] = s < a.splits ? *reinterpret_cast<const f32x4 *>(a.part + (s * total + r) * 4)
+                           : f32x4{-INFINITY, 0.f, -INFINITY, 0.f};
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-      sum[m] += st[s * total * 4 + 2 * m + 1] * __builtin_amdgcn_exp2f(st[s * total * 4 + 2 * m] - top[m]);
+      for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], st[i][2 * m]);
+    }
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], __shfl_xor(top[m], w, 64));
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        // a split without keys has nothing written: weight zero, and not read
+        const float by = st[i][2 * m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i][2 * m] - top[m]);
+        weight[m][i * 64 + tid] = by;
+        sum[m] += by * st[i][2 * m + 1];
+      }
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) sum[m] += __shfl_xor(sum[m], w, 64);
+  }
+  __syncthreads();
+  if (tid < 64) second[tid] = tid < 2 ? sum[tid] : 0.f;  // hand the sums to everybody
+  __syncthreads();
+  const float total_weight[2] = {second[0], second[1]};
+  __syncthreads();
+  const bool any = in && total_weight[0] > 0.f;
   const float lam = a.lam[head];
   T *o = static_cast<T *>(a.out) + clip * a.o_batch + query * a.o_pitch + static_cast<int64_t>(head) * 2 * a.d;
-  T *o2 = a.out2 ? static_cast<T *>(a.out2) +
-                       ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d
-                 : nullptr;
+  T *o2 = static_cast<T *>(a.out2) + ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;
   const float *part = a.part + a.splits * total * 4 + r * 4 * a.d;
-  for (int col = threadIdx.x; col < 2 * a.d; col += 64) {
-    float v[2] = {0.f, 0.f};
-    for (int s = 0; any && s < a.splits; ++s) {
-      if (st[s * total * 4 + 1] == 0.f) continue;  // this split saw no key
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-        v[m] += part[s * total * 4 * a.d + m * 2 * a.d + col] *
-                __builtin_amdgcn_exp2f(st[s * total * 4 + 2 * m] - top[m]);
+  const int64_t step = total * 4 * a.d;
+  // 128 columns at a time: one half of the threads sums the first map, one the second
+  for (int c0 = 0; c0 < 2 * a.d; c0 += 128) {
+    const int m = tid >> 7, col = c0 + (tid & 127);
+    float v = 0.f;
+    if (any && col < 2 * a.d) {
+      const float *p = part + m * 2 * a.d + col;
+#pragma unroll 8
+      for (int s = 0; s < a.splits; ++s) {
+        const float by = weight[m][s];
+        if (by != 0.f) v += by * p[s * step];
+      }
+      v /= total_weight[m];
     }
-    const float second = any ? v[1] / sum[1] : 0.f;
-    o[col] = static_cast<T>(any ? v[0] / sum[0] - lam * second : 0.f);
-    if (o2) o2[col] = static_cast<T>(second);
+    if (m) second[tid & 127] = v;
+    __syncthreads();
+    if (!m && col < 2 * a.d) {
+      const float w = second[tid & 127];
+      o[col] = static_cast<T>(v - lam * w);
+      if (a.out2) o2[col] = static_cast<T>(w);
+    }
+    __syncthreads();
   }
-  if (a.lse && threadIdx.x < 2) {
-    const int m = threadIdx.x;
+  if (a.lse && tid < 2) {
     const int64_t at = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
-    a.lse[m * static_cast<int64_t>(a.n) * a.hq * a.lq + at] = any ? top[m] + log2f(sum[m]) : INFINITY;
+    a.lse[tid * static_cast<int64_t>(a.n) * a.hq * a.lq + at] =
+        any ? top[tid] + log2f(total_weight[tid]) : INFINITY;
   }
 }
 
@@ -304,14 +340,15 @@ int fwd(const AttnArgs &a, hipStream_t s) {
   if (e != hipSuccess) return e;
   attn_fwd_kernel<T, D, ROWS, SPLIT><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
   if (SPLIT)
-    attn_join_kernel<T><<<static_cast<unsigned>(static_cast<int64_t>(a.n) * a.hk * a.lq * a.group), 64, 0, s>>>(a);
+    attn_join_kernel<T><<<static_cast<unsigned>(static_cast<int64_t>(a.n) * a.hk * a.lq * a.group), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 int fwd_shape(const AttnArgs &a, int rows, hipStream_t s) {
+  constexpr int kMost = attn_row_groups(D);
   if (rows == 1) return a.splits > 1 ? fwd<T, D, 1, true>(a, s) : fwd<T, D, 1, false>(a, s);
-  return fwd<T, D, attn_row_groups(D), false>(a, s);
+  return a.splits > 1 ? fwd<T, D, kMost, true>(a, s) : fwd<T, D, kMost, false>(a, s);
 }
 
 template <typename T>

@@ -26,7 +26,8 @@ struct Dq {
 
 // Rows of queries as in the forward pass (a lane holds a row): S^T = K Q^T and
 // dP^T = V dO^T leave dS^T where the product dQ^T += K^T dS^T takes it.
-template <typename T, int D, int WAVES>
+// SPLIT: the keys are split over workgroups, which leave 32-bit partial gradients.
+template <typename T, int D, int WAVES, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn_dq_kernel(AttnArgs a) {
   using F = Dq<T, D, WAVES>;
   using KV = typename F::KV;
@@ -36,6 +37,8 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
 
   int64_t id = logical_block(a.blocks);
   if (id >= a.blocks) return;
+  const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
+  if (SPLIT) id /= a.splits;
   const int tile = a.tiles - 1 - static_cast<int>(id % a.tiles);
   id /= a.tiles;
   const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
@@ -47,7 +50,8 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   const bool in = row < used;
   const int limit = in ? visible(query, q_len, k_len, a.frame) : 0x7fffffff;
   const int last_block = min(used, (tile + 1) * WAVES * 32) - 1, last_wave = min(used, first + 32) - 1;
-  const int end = last_block < tile * WAVES * 32 ? 0 : visible(last_block / a.group, q_len, k_len, a.frame);
+  const int all = last_block < tile * WAVES * 32 ? 0 : visible(last_block / a.group, q_len, k_len, a.frame);
+  const int begin = SPLIT ? split * a.span : 0, end = SPLIT ? min(all, begin + a.span) : all;
   const int wave_end = last_wave < first ? 0 : visible(last_wave / a.group, q_len, k_len, a.frame);
   const int whole = last_wave < first ? 0 : visible(first / a.group, q_len, k_len, a.frame);
 
@@ -57,7 +61,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   f32x16 acc[2][D / 32] = {};
   float dl = 0.f;
 
-  if (end > 0) {
+  if (begin < end) {
     Frag<T> q[2][D / 16], g[2 * D / 16];
     float lse[2] = {INFINITY, INFINITY}, mean[2] = {0.f, 0.f};
     {
@@ -93,7 +97,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       if (in) {
         lse[0] = a.lse[stat];
         lse[1] = a.lse[map + stat];
-        if (half == 0) {
+        if (half == 0 && begin == 0) {
           a.rowstat[stat] = mean[0];
           a.rowstat[map + stat] = mean[1];
         }
@@ -109,9 +113,9 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       KV::stage(k + key * a.k_pitch, n, a.d, a.k_pitch, k_off, lds + buf * 2 * KV::kBytes);
       KV::stage(v + key * a.v_pitch, n, a.d, a.v_pitch, v_off, lds + (buf * 2 + 1) * KV::kBytes);
     };
-    stage(0, 0);
+    stage(begin, 0);
     int buf = 0;
-    for (int key = 0; key < end; key += kKeys, buf ^= 1) {
+    for (int key = begin; key < end; key += kKeys, buf ^= 1) {
       tile_barrier();
       if (key + kKeys < end) stage(key + kKeys, buf ^ 1);
       if (key >= wave_end) continue;
@@ -131,12 +135,14 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
             for (int i = 0; i < 16; ++i)
               if (key + j + result_row(i, half) >= limit) s[i] = -INFINITY;
           }
+          float part = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float p = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -lse[m]));
-            if (m) dl += p * dp[i];
+            if (m) part += p * dp[i];  // short chains: the sum over a long row keeps its digits
             s[i] = p * (dp[i] - mean[m]);
           }
+          if (m) dl += part;
           // the softmax of a single key does not move (its row sum is exact here)
           if (masked && limit <= 1) s = f32x16{};
           const Frag<T> lo = pack<T>(s, 0), hi = pack<T>(s, 8);
@@ -152,10 +158,28 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   if (row >= rows) return;
   dl = half_sum(dl);
   if (half == 0) {
-    a.rowstat[2 * map + stat] = dl;
-    if (end <= 0) a.rowstat[stat] = a.rowstat[map + stat] = 0.f;
+    a.rowstat[(2 + split) * map + stat] = dl;
+    if (begin == 0 && end <= 0) a.rowstat[stat] = a.rowstat[map + stat] = 0.f;
   }
   if (!a.dq) return;
+  if constexpr (SPLIT) {
+    float *p = a.part + (split * map + (static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float by = m ? -lam * a.scale : a.scale;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int col = t * 32 + 8 * r + 4 * half;
+          if (col < a.d)
+            *reinterpret_cast<f32x4 *>(p + m * a.d + col) =
+                f32x4{acc[m][t][4 * r] * by, acc[m][t][4 * r + 1] * by, acc[m][t][4 * r + 2] * by,
+                      acc[m][t][4 * r + 3] * by};
+        }
+    }
+    return;
+  }
   T *dq = static_cast<T *>(a.dq) + clip * a.dq_batch + query * a.dq_pitch + static_cast<int64_t>(head) * 2 * a.d;
   struct alignas(4 * sizeof(T)) Four {
     T v[4];
@@ -196,7 +220,9 @@ struct Dkv {
   static constexpr int kLds = 2 * kBuffer + (kLdsK ? K::kBytes : 0);
 };
 
-template <typename T, int D, int WAVES>
+// SPLIT: the query tiles of a key head (its group's heads, one after another) are
+// split over workgroups, which leave 32-bit partial gradients.
+template <typename T, int D, int WAVES, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void attn_dkv_kernel(AttnArgs a) {
   using F = Dkv<T, D, WAVES>;
   using Q = typename F::Q;
@@ -206,6 +232,8 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
 
   int64_t id = logical_block(a.blocks);
   if (id >= a.blocks) return;
+  const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
+  if (SPLIT) id /= a.splits;
   const int tile = static_cast<int>(id % a.tiles);  // keys that most queries see first
   id /= a.tiles;
   const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
@@ -224,7 +252,14 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
   f32x16 dk[2][D / 32] = {}, dv[2 * D / 32] = {};
   const int begin = max(0, first_query(key_block)) / kRows * kRows;
 
-  if (key_block < k_len && begin < q_len) {
+  // query tiles that see the workgroup's keys, a group's heads after one another,
+  // and this split's share of them
+  const int per_head = key_block < k_len && begin < q_len ? (q_len - begin + kRows - 1) / kRows : 0;
+  const int total = per_head * a.group;
+  const int from_tile = SPLIT ? static_cast<int>(static_cast<int64_t>(total) * split / a.splits) : 0;
+  const int to_tile = SPLIT ? static_cast<int>(static_cast<int64_t>(total) * (split + 1) / a.splits) : total;
+
+  if (from_tile < to_tile) {
     const T *k = static_cast<const T *>(a.k) + clip * a.k_batch + (in ? key : 0) * a.k_pitch +
                  static_cast<int64_t>(kvh) * 2 * a.d;
     const T *v = static_cast<const T *>(a.v) + clip * a.v_batch + (in ? key : 0) * a.v_pitch +
@@ -258,11 +293,11 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
     Q::template offsets<true>(a.d, a.q_pitch, q_off);
     Q::template offsets<false>(a.d, a.do_pitch, g_off);
     const int64_t map = static_cast<int64_t>(a.n) * a.hq * a.lq;
-    const int per_head = (q_len - begin + kRows - 1) / kRows, total = per_head * a.group;
     const T *q = static_cast<const T *>(a.q) + clip * a.q_batch;
     const T *go = static_cast<const T *>(a.d_o) + clip * a.do_batch;
     // tile t: rows of head t / per_head from begin + t % per_head * kRows on
-    int st_head = 0, st_row = begin;  // of the tile to be staged next
+    int head = from_tile / per_head, row0 = begin + (from_tile - head * per_head) * kRows;
+    int st_head = head, st_row = row0;  // of the tile to be staged next
     auto stage = [&](int buf) {
       const int head = kvh * a.group + st_head, n = min(kRows, q_len - st_row);
       lds_char *to = lds + buf * F::kBuffer;
@@ -286,10 +321,10 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       }
     };
     stage(0);
-    int buf = 0, head = 0, row0 = begin;
-    for (int t = 0; t < total; ++t, buf ^= 1) {
+    int buf = 0;
+    for (int t = from_tile; t < to_tile; ++t, buf ^= 1) {
       tile_barrier();
-      if (t + 1 < total) stage(buf ^ 1);
+      if (t + 1 < to_tile) stage(buf ^ 1);
       const float lam = a.lam[kvh * a.group + head];
       const int at = row0;
       if ((row0 += kRows) >= q_len) {
@@ -366,6 +401,32 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
     }
   }
   if (key >= a.lk) return;
+  if constexpr (SPLIT) {
+    float *p = a.part + ((split * static_cast<int64_t>(a.n) + clip) * a.lk + key) * a.hk * 4 * a.d +
+               static_cast<int64_t>(kvh) * 4 * a.d;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int col = t * 32 + 8 * r + 4 * half;
+          if (col < a.d)
+            *reinterpret_cast<f32x4 *>(p + m * a.d + col) =
+                f32x4{dk[m][t][4 * r] * a.scale, dk[m][t][4 * r + 1] * a.scale, dk[m][t][4 * r + 2] * a.scale,
+                      dk[m][t][4 * r + 3] * a.scale};
+        }
+#pragma unroll
+    for (int t = 0; t < 2 * D / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int col = t * 32 + 8 * r + 4 * half;
+        if (col < 2 * a.d)
+          *reinterpret_cast<f32x4 *>(p + 2 * a.d + col) =
+              f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]};
+      }
+    return;
+  }
   struct alignas(4 * sizeof(T)) Four {
     T v[4];
   };
@@ -401,64 +462,139 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
   }
 }
 
-// dlambda of a head: its rows' sums, in a fixed order.
-__global__ __launch_bounds__(256) void attn_dlam_kernel(AttnArgs a) {
-  __shared__ float lds[256];
+// Adds up the splits' partial gradients in their order: a thread per four columns.
+// KEYS: dk and dv ([n][lk][hk][4 d]), else dq ([n][lq][hq][2 d]).  Rows behind a
+// clip's end are zero, whatever their partial results.
+template <typename T, bool KEYS>
+__global__ __launch_bounds__(256) void attn_sum_kernel(AttnArgs a) {
+  const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int per = (KEYS ? 4 : 2) * a.d / 4, heads = KEYS ? a.hk : a.hq, len = KEYS ? a.lk : a.lq;
+  const int64_t rows = static_cast<int64_t>(a.n) * len * heads;
+  if (id >= rows * per) return;
+  const int64_t row = id / per;
+  int col = static_cast<int>(id - row * per) * 4;
+  const int head = static_cast<int>(row % heads);
+  const int64_t token = row / heads;
+  const int clip = static_cast<int>(token / len), at = static_cast<int>(token - static_cast<int64_t>(clip) * len);
+  const bool in = at < clip_length(KEYS ? a.k_len : a.q_len, clip, len);
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (in) {
+    const float *p = a.part + id * 4;
+#pragma unroll 4
+    for (int i = 0; i < a.splits; ++i) {
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(p + i * rows * per * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
+  }
+  struct alignas(4 * sizeof(T)) Four {
+    T v[4];
+  } x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x.v[e] = static_cast<T>(s[e]);
+  T *out;
+  if constexpr (KEYS) {
+    if (col < 2 * a.d) {
+      out = static_cast<T *>(a.dk) + clip * a.dk_batch + at * a.dk_pitch;
+      if (!a.dk) return;
+    } else {
+      out = static_cast<T *>(a.dv) + clip * a.dv_batch + at * a.dv_pitch;
+      col -= 2 * a.d;
+      if (!a.dv) return;
+    }
+  } else {
+    out = static_cast<T *>(a.dq) + clip * a.dq_batch + at * a.dq_pitch;
+  }
+  *reinterpret_cast<Four *>(out + static_cast<int64_t>(head) * 2 * a.d + col) = x;
+}
+
+// dlambda of a head: its rows' sums over the clips and splits, in a fixed order.
+__global__ __launch_bounds__(1024) void attn_dlam_kernel(AttnArgs a) {
+  __shared__ float lds[16];
   const int head = blockIdx.x;
   const float *p = a.rowstat + 2 * static_cast<int64_t>(a.n) * a.hq * a.lq;
   float s = 0.f;
-  for (int clip = 0; clip < a.n; ++clip) {
-    const float *r = p + (static_cast<int64_t>(clip) * a.hq + head) * a.lq;
+  for (int64_t i = 0; i < static_cast<int64_t>(a.splits) * a.n; ++i) {
+    const float *r = p + (i * a.hq + head) * a.lq;
 #pragma unroll 4
-    for (int i = threadIdx.x; i < a.lq; i += 256) s += r[i];
+    for (int j = threadIdx.x; j < a.lq; j += 1024) s += r[j];
   }
-  lds[threadIdx.x] = s;
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
   __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if (static_cast<int>(threadIdx.x) < w) lds[threadIdx.x] += lds[threadIdx.x + w];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) a.dlam[head] = 0.f - lds[0];
+  if (threadIdx.x) return;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) s += lds[w];
+  a.dlam[head] = 0.f - s;
 }
 
-template <typename T, int D, int WAVES>
-int bwd(AttnArgs a, hipStream_t s) {
-  using A = Dq<T, D, WAVES>;
-  using B = Dkv<T, D, WAVES>;
-  const int64_t pairs = static_cast<int64_t>(a.n) * a.hk;
-  int e = allow_lds<attn_dq_kernel<T, D, WAVES>>(A::kLds);
-  if (e == hipSuccess) e = allow_lds<attn_dkv_kernel<T, D, WAVES>>(B::kLds);
+template <typename T, int D, bool SPLIT>
+int launch_dq(AttnArgs a, const BwdPlan &p, hipStream_t s) {
+  constexpr int kWaves = kBwdRows / 32;
+  using F = Dq<T, D, kWaves>;
+  const int e = allow_lds<attn_dq_kernel<T, D, kWaves, SPLIT>>(F::kLds);
   if (e != hipSuccess) return e;
-  a.tiles = (a.lq * a.group + 32 * WAVES - 1) / (32 * WAVES);
-  a.blocks = pairs * a.tiles;
-  if (a.blocks) attn_dq_kernel<T, D, WAVES><<<grid_of(a.blocks), A::kThreads, A::kLds, s>>>(a);
-  a.tiles = (a.lk + 32 * WAVES - 1) / (32 * WAVES);
-  a.blocks = pairs * a.tiles;
-  if (a.blocks && (a.dk || a.dv))
-    attn_dkv_kernel<T, D, WAVES><<<grid_of(a.blocks), B::kThreads, B::kLds, s>>>(a);
-  if (a.dlam) attn_dlam_kernel<<<a.hq, 256, 0, s>>>(a);
+  a.tiles = (a.lq * a.group + kBwdRows - 1) / kBwdRows;
+  a.splits = p.dq_splits;
+  a.span = p.dq_span;
+  a.blocks = static_cast<int64_t>(a.n) * a.hk * a.tiles * a.splits;
+  a.part = a.rowstat + p.dq_part;
+  if (a.blocks == 0) return hipSuccess;
+  attn_dq_kernel<T, D, kWaves, SPLIT><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
+  if (SPLIT && a.dq) {
+    const int64_t threads = static_cast<int64_t>(a.n) * a.lq * a.hq * a.d / 2;
+    attn_sum_kernel<T, false><<<static_cast<unsigned>((threads + 255) / 256), 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, int D, bool SPLIT>
+int launch_dkv(AttnArgs a, const BwdPlan &p, hipStream_t s) {
+  constexpr int kWaves = kBwdRows / 32;
+  using F = Dkv<T, D, kWaves>;
+  const int e = allow_lds<attn_dkv_kernel<T, D, kWaves, SPLIT>>(F::kLds);
+  if (e != hipSuccess) return e;
+  a.tiles = (a.lk + kBwdRows - 1) / kBwdRows;
+  a.splits = p.dkv_splits;
+  a.blocks = static_cast<int64_t>(a.n) * a.hk * a.tiles * a.splits;
+  a.part = a.rowstat + p.dkv_part;
+  if (a.blocks == 0) return hipSuccess;
+  attn_dkv_kernel<T, D, kWaves, SPLIT><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
+  if (SPLIT) {
+    const int64_t threads = static_cast<int64_t>(a.n) * a.lk * a.hk * a.d;
+    attn_sum_kernel<T, true><<<static_cast<unsigned>((threads + 255) / 256), 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
 template <typename T, int D>
-int bwd_waves(const AttnArgs &a, hipStream_t s) {
-  return bwd<T, D, 4>(a, s);
+int bwd(const AttnArgs &a, const BwdPlan &p, hipStream_t s) {
+  int e = p.dq_splits > 1 ? launch_dq<T, D, true>(a, p, s) : launch_dq<T, D, false>(a, p, s);
+  if (e == hipSuccess && (a.dk || a.dv))
+    e = p.dkv_splits > 1 ? launch_dkv<T, D, true>(a, p, s) : launch_dkv<T, D, false>(a, p, s);
+  if (e != hipSuccess || !a.dlam) return e;
+  AttnArgs l = a;
+  l.splits = p.dq_splits;
+  attn_dlam_kernel<<<a.hq, 1024, 0, s>>>(l);
+  return hipGetLastError();
 }
 
 template <typename T>
-int bwd_type(const AttnArgs &a, hipStream_t s) {
-  if (a.d <= 32) return bwd_waves<T, 32>(a, s);
-  if (a.d <= 64) return bwd_waves<T, 64>(a, s);
-  return bwd_waves<T, 128>(a, s);
+int bwd_type(const AttnArgs &a, const BwdPlan &p, hipStream_t s) {
+  if (a.d <= 32) return bwd<T, 32>(a, p, s);
+  if (a.d <= 64) return bwd<T, 64>(a, p, s);
+  return bwd<T, 128>(a, p, s);
 }
 
 }  // namespace
 
-int launch_attn_bwd(const AttnArgs &a, int dtype, void *stream) {
+int launch_attn_bwd(const AttnArgs &a, const BwdPlan &p, int dtype, void *stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == RT3D_F32) return bwd_type<float>(a, s);
-  if (dtype == RT3D_BF16) return bwd_type<__bf16>(a, s);
-  return bwd_type<_Float16>(a, s);
+  if (dtype == RT3D_F32) return bwd_type<float>(a, p, s);
+  if (dtype == RT3D_BF16) return bwd_type<__bf16>(a, p, s);
+  return bwd_type<_Float16>(a, p, s);
 }
 
 }  // namespace rt3d

@@ -15,6 +15,8 @@ constexpr int64_t kMaxBlocks = (1ll << 31) - 16;
 constexpr int kMaxNormColumns = 1 << 20;
 constexpr int64_t kMaxPitch = 1 << 22;   // elements: a tile's rows stay within 2^31 bytes
 constexpr int kMaxLength = 1 << 30;
+constexpr int kSplitBlocks = 2048;   // workgroups of one wave that a call of few queries is split into
+constexpr int kSplitKeys = 256;      // least keys of such a split
 
 bool known_dtype(int dtype) { return dtype == RT3D_F32 || dtype == RT3D_BF16 || dtype == RT3D_F16; }
 int esize(int dtype) { return dtype == RT3D_F32 ? 4 : 2; }
@@ -175,6 +177,36 @@ AttnArgs attn_args(const rt3d_diffattn_desc *d, const Shape &s) {
   return a;
 }
 
+// How many parts a workgroup's walk is split into.  blocks: workgroups of a call
+// without splits, each a walk of `steps` steps of `step_us` on a CU of its own;
+// part_bytes: one split's partial results, written and read once at 4 TB/s; a
+// split call pays 5 us for its second launch.  The time is that of the fullest
+// CU; more than one workgroup on a CU run at 0.6 of the sum of their times.
+constexpr int kCus = 256;
+int pick_splits(int64_t blocks, int64_t steps, double step_us, double part_bytes, int64_t most) {
+  if (blocks <= 0 || blocks >= 2 * kCus || steps < 2) return 1;
+  auto time = [&](int64_t s) {
+    const double on_cu = static_cast<double>((blocks * s + kCus - 1) / kCus);
+    const double walk = static_cast<double>((steps + s - 1) / s) * step_us;
+    return walk * std::max(1.0, 0.6 * on_cu) + (s > 1 ? 5.0 + 2 * s * part_bytes / 4e6 : 0.0);
+  };
+  int best = 1;
+  for (int64_t s = 2; s <= most && s <= steps; ++s)
+    if (time(s) < time(best)) best = static_cast<int>(s);
+  return best;
+}
+
+// Keys of a split: whole staged tiles (of 32 or 64 keys), so that none reaches into the next.
+int split_span(int lk, int splits) { return static_cast<int>((static_cast<int64_t>(lk) + splits - 1) / splits + 63) / 64 * 64; }
+
+// Time of a step of 32 keys (forward, dq) or 32 queries (dk, dv) of a workgroup
+// alone on its CU, in us per 32 channels of d: 16-bit products are issued in a
+// sixteenth of the time of 32-bit ones.
+double step_us(const rt3d_diffattn_desc *d, double bits16, double bits32) {
+  const int wide = d->d <= 32 ? 1 : d->d <= 64 ? 2 : 4;
+  return wide * (d->dtype == RT3D_F32 ? bits32 : bits16);
+}
+
 // Launch of a forward call: groups of 32 rows of a workgroup and splits of the keys.
 struct FwdPlan {
   int row_groups, tiles, splits, span;
@@ -182,36 +214,57 @@ struct FwdPlan {
   uint64_t bytes;  // workspace
 };
 
-constexpr int kFillBlocks = 512;     // two workgroups of four waves on each of 256 CUs
-constexpr int kSplitBlocks = 2048;   // single waves, when keys are split
-constexpr int kSplitKeys = 256;      // least keys of a split
-
 FwdPlan fwd_plan(const rt3d_diffattn_desc *d, const Shape &s, uint64_t workspace) {
   FwdPlan p{};
   const int64_t rows = static_cast<int64_t>(d->lq) * s.group, pairs = static_cast<int64_t>(d->n) * d->hk;
-  const int most = attn_row_groups(d->d);
-  auto tiles = [&](int groups) { return static_cast<int>((rows + 32 * groups - 1) / (32 * groups)); };
+  // One group where more would leave waves without rows: then a workgroup is one
+  // wave (two beyond d = 64) and a CU holds several.
+  p.row_groups = rows <= 32 ? 1 : attn_row_groups(d->d);
+  p.tiles = static_cast<int>((rows + 32 * p.row_groups - 1) / (32 * p.row_groups));
+  p.blocks = pairs * p.tiles;
   p.splits = 1;
   p.span = d->lk;
-  p.row_groups = pairs * tiles(most) >= kFillBlocks ? most : 1;
-  p.tiles = tiles(p.row_groups);
-  p.blocks = pairs * p.tiles;
-  if (p.row_groups == 1 && p.blocks > 0) {
-    const uint64_t one = static_cast<uint64_t>(pairs * rows) * (4 + 4 * d->d) * sizeof(float);
-    int64_t splits = std::min<int64_t>(kSplitBlocks / p.blocks, d->lk / kSplitKeys);
-    splits = std::min<int64_t>(splits, static_cast<int64_t>(workspace / std::max<uint64_t>(one, 1)));
-    if (splits > 1) {
-      p.span = static_cast<int>(((d->lk + splits - 1) / splits + 31) / 32 * 32);
-      p.splits = (d->lk + p.span - 1) / p.span;
-      p.blocks *= p.splits;
-      p.bytes = one * p.splits;
-    }
+  const uint64_t one = static_cast<uint64_t>(pairs * rows) * (4 + 4 * d->d) * sizeof(float);
+  if (p.blocks <= 0) return p;
+  const int64_t most = std::min<int64_t>(256, static_cast<int64_t>(workspace / one));
+  int64_t splits;
+  if (p.row_groups == 1) {
+    // bound by the cache's bytes: enough waves to keep them coming
+    splits = std::min<int64_t>({most, kSplitBlocks / p.blocks, d->lk / kSplitKeys});
+  } else {
+    splits = pick_splits(p.blocks, (d->lk + 31) / 32, step_us(d, 0.35, 1.3), static_cast<double>(one), most);
+  }
+  if (splits > 1) {
+    p.span = split_span(d->lk, static_cast<int>(splits));
+    p.splits = (d->lk + p.span - 1) / p.span;
+  }
+  if (p.splits > 1) {
+    p.blocks *= p.splits;
+    p.bytes = one * p.splits;
   }
   return p;
 }
 
-uint64_t bwd_workspace(const rt3d_diffattn_desc *d) {
-  return 3ull * d->n * d->hq * d->lq * sizeof(float);
+BwdPlan bwd_plan(const rt3d_diffattn_desc *d, const Shape &s) {
+  BwdPlan p{};
+  const int64_t rows = static_cast<int64_t>(d->lq) * s.group, pairs = static_cast<int64_t>(d->n) * d->hk;
+  const uint64_t stats = static_cast<uint64_t>(d->n) * d->hq * d->lq;
+  const uint64_t dq = stats * 2 * d->d, dkv = static_cast<uint64_t>(pairs) * d->lk * 4 * d->d;
+  p.dq_span = d->lk;
+  p.dq_splits = pick_splits(pairs * ((rows + kBwdRows - 1) / kBwdRows), (d->lk + 31) / 32,
+                            step_us(d, 0.35, 1.3), dq * 4.0, 16);
+  if (p.dq_splits > 1) {
+    p.dq_span = split_span(d->lk, p.dq_splits);
+    p.dq_splits = (d->lk + p.dq_span - 1) / p.dq_span;
+  }
+  p.dkv_splits = pick_splits(pairs * ((d->lk + kBwdRows - 1) / kBwdRows),
+                             static_cast<int64_t>(s.group) * ((d->lq + 31) / 32), step_us(d, 0.45, 1.8),
+                             dkv * 4.0, 16);
+  auto up = [](uint64_t floats) { return (floats + 3) / 4 * 4; };  // parts begin at 16 bytes
+  p.dq_part = up((2 + p.dq_splits) * stats);
+  p.dkv_part = p.dq_part + (p.dq_splits > 1 ? up(p.dq_splits * dq) : 0);
+  p.floats = p.dkv_part + (p.dkv_splits > 1 ? p.dkv_splits * dkv : 0);
+  return p;
 }
 
 }  // namespace
@@ -380,7 +433,7 @@ rt3d_status rt3d_diffattn_bwd_workspace_size(const rt3d_diffattn_desc *d, uint64
   const rt3d_status st = check_attn(d, true, s);
   if (st != RT3D_OK) return st;
   if (!bytes) return fail(RT3D_ERR_INVALID_ARG, "bytes must be non-NULL");
-  *bytes = bwd_workspace(d);
+  *bytes = bwd_plan(d, s).floats * sizeof(float);
   return ok();
 }
 
@@ -396,12 +449,13 @@ rt3d_status rt3d_diffattn_bwd(const rt3d_diffattn_desc *d, const void *q, const 
   if (queries && (!q || !lambda || !o || !o2 || !lse || !d_o))
     return fail(RT3D_ERR_INVALID_ARG, "q, lambda, o, o2, lse and d_o must be non-NULL");
   if (keys && (!k || !v)) return fail(RT3D_ERR_INVALID_ARG, "k and v must be non-NULL");
-  for (const void *p : {q, k, v, o, o2, d_o, static_cast<const void *>(dq), static_cast<const void *>(dk),
+  for (const void *x : {q, k, v, o, o2, d_o, static_cast<const void *>(dq), static_cast<const void *>(dk),
                         static_cast<const void *>(dv), static_cast<const void *>(workspace)})
-    if (!aligned(p, 16)) return fail(RT3D_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
+    if (!aligned(x, 16)) return fail(RT3D_ERR_INVALID_ARG, "device pointers must be 16-byte aligned");
   if (!aligned(lambda, 4) || !aligned(lse, 4) || !aligned(dlambda, 4) || !aligned(q_len, 4) || !aligned(k_len, 4))
     return fail(RT3D_ERR_INVALID_ARG, "lambda, dlambda, lse and lengths must be 4-byte aligned");
-  const uint64_t need = bwd_workspace(d);
+  const BwdPlan p = bwd_plan(d, s);
+  const uint64_t need = p.floats * sizeof(float);
   if (need && (!workspace || workspace_bytes < need))
     return fail(RT3D_ERR_BUFFER_TOO_SMALL, "the backward pass needs %llu bytes of workspace, got %llu",
                 static_cast<unsigned long long>(need),
@@ -422,7 +476,7 @@ rt3d_status rt3d_diffattn_bwd(const rt3d_diffattn_desc *d, const void *q, const 
   a.dv = dv;
   a.dlam = dlambda;
   a.rowstat = static_cast<float *>(workspace);
-  return launched(launch_attn_bwd(a, d->dtype, stream));
+  return launched(launch_attn_bwd(a, p, d->dtype, stream));
 }
 
 }  // extern "C"

@@ -47,7 +47,7 @@ struct AttnArgs {
   float *lse;                 // [2][n][hq][lq], base-2 logarithms (forward writes, or NULL)
   const int32_t *q_len, *k_len;
   float *part;                // partial results of split calls
-  float *rowstat;             // backward: [2][n][hq][lq] row sums, then [n][hq][lq] sums of P_2 dP
+  float *rowstat;             // backward: [2][n][hq][lq] row sums, then [dq splits][n][hq][lq] sums of P_2 dP
   float *dlam;                // [hq]
   int64_t q_pitch, k_pitch, v_pitch, o_pitch;
   int64_t q_batch, k_batch, v_batch, o_batch;
@@ -71,6 +71,14 @@ int launch_rope(const RopeArgs &a, int dtype, int halves, int pairs, void *strea
 // Groups of 32 rows that a workgroup of a call without splits holds, 1 or this.
 constexpr int attn_row_groups(int d) { return d > 64 ? 2 : 4; }
 int launch_attn_fwd(const AttnArgs &a, int dtype, int row_groups, void *stream);
-int launch_attn_bwd(const AttnArgs &a, int dtype, void *stream);
+
+// Splits of the backward kernels' walks (keys for dq, query tiles for dk and dv),
+// and where their partial results lie in the workspace (floats).
+struct BwdPlan {
+  int dq_splits, dq_span, dkv_splits, dkv_span;
+  uint64_t dq_part, dkv_part, floats;
+};
+constexpr int kBwdRows = 128;  // rows (keys) of a backward workgroup
+int launch_attn_bwd(const AttnArgs &a, const BwdPlan &p, int dtype, void *stream);
 
 }  // namespace rt3d
