@@ -458,9 +458,7 @@ typedef struct {
 
 /* pos: int32 [n][t*h*w][3] device array of (time, row, column) per token, any
  * values, or NULL: the token's place in the grid, time from t0 on.  y may be x
- * with one layout (in place); otherwise they must not overlap.  Pairs of
- * neighbours need even pitches and batch strides and pointers aligned to a pair
- * (RT3D_ERR_UNSUPPORTED). */
+ * with one layout (in place); otherwise they must not overlap. */
 rt3d_status rt3d_rope3d(const rt3d_rope_desc *desc, const void *x, const int32_t *pos, void *y,
                         void *stream);
 

@@ -250,86 +250,110 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
   }
 }
 
-// Joins the splits of a row in their order.  A workgroup per row: the splits'
-// weights first (one thread each), then a thread per map and column.
+// Joins the splits of a row in their order.  SHARE waves per row: each finds the
+// splits' weights (a lane per split), sums its share of them with half of its
+// lanes per map and four columns per lane, and the shares meet in LDS.
 constexpr int kMaxSplits = 256;
-template <typename T>
+template <typename T, int SHARE>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  __shared__ float weight[2][kMaxSplits], second[256];
-  const int rows = a.lq * a.group, tid = threadIdx.x;
-  const int64_t r = blockIdx.x, total = static_cast<int64_t>(a.n) * a.hk * rows;
+  constexpr int kPer = kMaxSplits / 64;
+  __shared__ f32x4 shared[SHARE > 1 ? SHARE - 1 : 1][64];
+  const int rows = a.lq * a.group, lane = threadIdx.x & 63, wave = uniform(static_cast<int>(threadIdx.x) >> 6);
+  const int64_t total = static_cast<int64_t>(a.n) * a.hk * rows;
+  const int64_t r = SHARE > 1 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
+  const int share = SHARE > 1 ? wave : 0;
+  if (r >= total) return;
   const int row = static_cast<int>(r % rows);
   const int64_t pair = r / rows;
   const int kvh = static_cast<int>(pair % a.hk), clip = static_cast<int>(pair / a.hk);
   const int query = row / a.group, head = kvh * a.group + (row - query * a.group);
   const bool in = query < clip_length(a.q_len, clip, a.lq);
-  // a wave's lanes take splits lane, lane + 64, ...: four at most
-  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-  if (in && tid < 64) {
-    f32x4 st[kMaxSplits / 64];
+  float weight[2][kPer], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+  f32x4 st[kPer];
 #pragma unroll
-    for (int i = 0; i < kMaxSplits / 64; ++i) {
-      const int s = i * 64 + tid;
-      st[i] = s < a.splits ? *reinterpret_cast<const f32x4 *>(a.part + (s * total + r) * 4)
-                           : f32x4{-INFINITY, 0.f, -INFINITY, 0.f};
+  for (int i = 0; i < kPer; ++i) {
+    const int s = i * 64 + lane;
+    st[i] = f32x4{-INFINITY, 0.f, -INFINITY, 0.f};
+    if (in && s < a.splits) st[i] = *reinterpret_cast<const f32x4 *>(a.part + (s * total + r) * 4);
 #pragma unroll
-      for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], st[i][2 * m]);
+    for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], st[i][2 * m]);
+  }
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], __shfl_xor(top[m], w, 64));
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      // a split without keys has weight zero: its results were not written and are not used
+      weight[m][i] = st[i][2 * m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i][2 * m] - top[m]);
+      sum[m] += weight[m][i] * st[i][2 * m + 1];
     }
 #pragma unroll
-    for (int w = 32; w > 0; w >>= 1)
+  for (int w = 32; w > 0; w >>= 1)
 #pragma unroll
-      for (int m = 0; m < 2; ++m) top[m] = fmaxf(top[m], __shfl_xor(top[m], w, 64));
-#pragma unroll
-    for (int i = 0; i < kMaxSplits / 64; ++i)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        // a split without keys has nothing written: weight zero, and not read
-        const float by = st[i][2 * m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i][2 * m] - top[m]);
-        weight[m][i * 64 + tid] = by;
-        sum[m] += by * st[i][2 * m + 1];
-      }
-#pragma unroll
-    for (int w = 32; w > 0; w >>= 1)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) sum[m] += __shfl_xor(sum[m], w, 64);
-  }
-  __syncthreads();
-  if (tid < 64) second[tid] = tid < 2 ? sum[tid] : 0.f;  // hand the sums to everybody
-  __syncthreads();
-  const float total_weight[2] = {second[0], second[1]};
-  __syncthreads();
-  const bool any = in && total_weight[0] > 0.f;
+    for (int m = 0; m < 2; ++m) sum[m] += __shfl_xor(sum[m], w, 64);
+  const bool any = in && sum[0] > 0.f;
   const float lam = a.lam[head];
   T *o = static_cast<T *>(a.out) + clip * a.o_batch + query * a.o_pitch + static_cast<int64_t>(head) * 2 * a.d;
   T *o2 = static_cast<T *>(a.out2) + ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;
-  const float *part = a.part + a.splits * total * 4 + r * 4 * a.d;
+  const int m = lane >> 5;
+  const float *part = a.part + a.splits * total * 4 + r * 4 * a.d + m * 2 * a.d;
   const int64_t step = total * 4 * a.d;
-  // 128 columns at a time: one half of the threads sums the first map, one the second
+  struct alignas(4 * sizeof(T)) Four {
+    T v[4];
+  };
   for (int c0 = 0; c0 < 2 * a.d; c0 += 128) {
-    const int m = tid >> 7, col = c0 + (tid & 127);
-    float v = 0.f;
-    if (any && col < 2 * a.d) {
-      const float *p = part + m * 2 * a.d + col;
-#pragma unroll 8
-      for (int s = 0; s < a.splits; ++s) {
-        const float by = weight[m][s];
-        if (by != 0.f) v += by * p[s * step];
+    const int col = c0 + (lane & 31) * 4;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (any) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int n = min(64, a.splits - i * 64);
+        for (int s0 = share; s0 < n; s0 += 8 * SHARE) {
+          f32x4 x[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {  // eight loads in flight
+            const int s = min(s0 + j * SHARE, n - 1);
+            x[j] = *reinterpret_cast<const f32x4 *>(part + (i * 64 + s) * step + (col < 2 * a.d ? col : 0));
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int s = s0 + j * SHARE;
+            const float w0 = __shfl(weight[0][i], s, 64), w1 = __shfl(weight[1][i], s, 64), by = m ? w1 : w0;
+            if (s < n && w0 != 0.f) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] += by * x[j][e];
+            }
+          }
+        }
       }
-      v /= total_weight[m];
     }
-    if (m) second[tid & 127] = v;
-    __syncthreads();
-    if (!m && col < 2 * a.d) {
-      const float w = second[tid & 127];
-      o[col] = static_cast<T>(v - lam * w);
-      if (a.out2) o2[col] = static_cast<T>(w);
+    if constexpr (SHARE > 1) {
+      __syncthreads();
+      if (share) shared[share - 1][lane] = v;
+      __syncthreads();
+      if (share) continue;
+#pragma unroll
+      for (int s = 0; s < SHARE - 1; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += shared[s][lane][e];
     }
-    __syncthreads();
+    Four x, y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float mine = any ? v[e] / sum[m] : 0.f, other = __shfl_xor(mine, 32, 64);
+      x.v[e] = static_cast<T>(mine - lam * other);
+      y.v[e] = static_cast<T>(mine);
+    }
+    if (col >= 2 * a.d) continue;
+    if (m == 0) *reinterpret_cast<Four *>(o + col) = x;
+    if (m == 1 && a.out2) *reinterpret_cast<Four *>(o2 + col) = y;
   }
-  if (a.lse && tid < 2) {
+  if (a.lse && share == 0 && (lane & 31) == 0) {
     const int64_t at = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
-    a.lse[tid * static_cast<int64_t>(a.n) * a.hq * a.lq + at] =
-        any ? top[tid] + log2f(total_weight[tid]) : INFINITY;
+    a.lse[m * static_cast<int64_t>(a.n) * a.hq * a.lq + at] = any ? top[m] + log2f(sum[m]) : INFINITY;
   }
 }
 
@@ -339,8 +363,12 @@ int fwd(const AttnArgs &a, hipStream_t s) {
   const int e = allow_lds<attn_fwd_kernel<T, D, ROWS, SPLIT>>(F::kLds);
   if (e != hipSuccess) return e;
   attn_fwd_kernel<T, D, ROWS, SPLIT><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
-  if (SPLIT)
-    attn_join_kernel<T><<<static_cast<unsigned>(static_cast<int64_t>(a.n) * a.hk * a.lq * a.group), 256, 0, s>>>(a);
+  if (SPLIT) {
+    const int64_t rows = static_cast<int64_t>(a.n) * a.hk * a.lq * a.group;
+    // four waves share a row's splits where there are more than a few
+    if (a.splits > 16) attn_join_kernel<T, 4><<<static_cast<unsigned>(rows), 256, 0, s>>>(a);
+    else attn_join_kernel<T, 1><<<static_cast<unsigned>((rows + 3) / 4), 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 

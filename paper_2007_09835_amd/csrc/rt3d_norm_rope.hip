@@ -12,17 +12,29 @@
 namespace rt3d {
 namespace {
 
+// V elements in one access of up to 16 bytes, at any element's address (global
+// memory takes unaligned vectors; on this card they cost what their lines cost).
 template <typename T, int V>
-struct alignas(sizeof(T) * V) Pack {
+struct Pack {
   T v[V];
 };
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> get(const T *p) {
+  Pack<T, V> x;
+  __builtin_memcpy(&x, p, sizeof(x));
+  return x;
+}
+template <typename T, int V>
+__device__ __forceinline__ void put(T *p, const Pack<T, V> &x) {
+  __builtin_memcpy(p, &x, sizeof(x));
+}
 
 // V elements of a row from column `col` on, as floats; columns from c on are zero
 // and never read.
 template <typename T, int V>
 __device__ __forceinline__ void load_row(const T *p, int col, int c, float (&out)[V]) {
   if (col + V <= c) {
-    const Pack<T, V> x = *reinterpret_cast<const Pack<T, V> *>(p + col);
+    const Pack<T, V> x = get<T, V>(p + col);
 #pragma unroll
     for (int e = 0; e < V; ++e) out[e] = static_cast<float>(x.v[e]);
   } else {
@@ -37,7 +49,7 @@ __device__ __forceinline__ void store_row(T *p, int col, int c, const float (&in
     Pack<T, V> x;
 #pragma unroll
     for (int e = 0; e < V; ++e) x.v[e] = static_cast<T>(in[e]);
-    *reinterpret_cast<Pack<T, V> *>(p + col) = x;
+    put(p + col, x);
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
@@ -45,22 +57,48 @@ __device__ __forceinline__ void store_row(T *p, int col, int c, const float (&in
   }
 }
 
-// A weight vector's elements (any alignment of 4 bytes); `none` where it is absent.
+// A weight vector's elements; `none` where it is absent.
 template <int V>
 __device__ __forceinline__ void load_weight(const float *p, int col, int c, float none, float (&out)[V]) {
+  if (p) {
+    load_row(p, col, c, out);
+  } else {
 #pragma unroll
-  for (int e = 0; e < V; ++e) out[e] = p && col + e < c ? p[col + e] : none;
+    for (int e = 0; e < V; ++e) out[e] = none;
+  }
+}
+
+// The sum of a value over 2 S neighbouring lanes that hold equal sums over S.
+template <int S>
+__device__ __forceinline__ float lane_step(float v) {
+  const unsigned u = __float_as_uint(v);
+  if constexpr (S == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else if constexpr (S == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else {
+    // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
+    constexpr int kDpp = S == 1 ? 0xb1 : S == 2 ? 0x4e : S == 4 ? 0x141 : 0x140;
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, static_cast<int>(u), kDpp, 0xf, 0xf, true));
+  }
 }
 
 // Sums of N values over the LPR lanes of a row (a power of two up to 64, or the
-// whole workgroup of 256); every lane gets them.  The order is fixed.
+// whole workgroup of 256); every lane gets them.  The order is fixed; no step goes
+// through LDS but the last one of a workgroup.
 template <int LPR, int N>
 __device__ __forceinline__ void row_sum(float (&v)[N], float *lds) {
-  constexpr int kIn = LPR < 64 ? LPR : 64;
 #pragma unroll
-  for (int s = kIn / 2; s > 0; s >>= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], s, 64);
+  for (int i = 0; i < N; ++i) {
+    v[i] = lane_step<1>(v[i]);
+    v[i] = lane_step<2>(v[i]);
+    v[i] = lane_step<4>(v[i]);
+    if constexpr (LPR >= 16) v[i] = lane_step<8>(v[i]);
+    if constexpr (LPR >= 32) v[i] = lane_step<16>(v[i]);
+    if constexpr (LPR >= 64) v[i] = lane_step<32>(v[i]);
+  }
   if constexpr (LPR > 64) {
     const int wave = threadIdx.x >> 6;
     __syncthreads();  // the last sums have been read
@@ -130,8 +168,8 @@ __global__ __launch_bounds__(kNormThreads) void layernorm_fwd_kernel(NormArgs a)
   }
 }
 
-// Rows too long for registers (or whose alignment allows single elements only):
-// a workgroup reads a row three times, the second and third time from cache.
+// Rows too long for registers: a workgroup reads a row three times, the second and
+// third time from cache.
 template <typename T, int V>
 __global__ __launch_bounds__(kNormThreads) void layernorm_fwd_long_kernel(NormArgs a) {
   __shared__ float lds[8];
@@ -405,12 +443,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     T *yv = y + static_cast<int64_t>(v) * a.d;
     T p0[P], p1[P];
     if constexpr (HALVES) {
-      const Pack<T, P> u = *reinterpret_cast<const Pack<T, P> *>(xv + first);
-      const Pack<T, P> w = *reinterpret_cast<const Pack<T, P> *>(xv + second);
+      const Pack<T, P> u = get<T, P>(xv + first), w = get<T, P>(xv + second);
 #pragma unroll
       for (int j = 0; j < P; ++j) p0[j] = u.v[j], p1[j] = w.v[j];
     } else {
-      const Pack<T, 2 * P> u = *reinterpret_cast<const Pack<T, 2 * P> *>(xv + first);
+      const Pack<T, 2 * P> u = get<T, 2 * P>(xv + first);
 #pragma unroll
       for (int j = 0; j < P; ++j) p0[j] = u.v[2 * j], p1[j] = u.v[2 * j + 1];
     }
@@ -426,13 +463,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       Pack<T, P> u, w;
 #pragma unroll
       for (int j = 0; j < P; ++j) u.v[j] = p0[j], w.v[j] = p1[j];
-      *reinterpret_cast<Pack<T, P> *>(yv + first) = u;
-      *reinterpret_cast<Pack<T, P> *>(yv + second) = w;
+      put(yv + first, u);
+      put(yv + second, w);
     } else {
       Pack<T, 2 * P> u;
 #pragma unroll
       for (int j = 0; j < P; ++j) u.v[2 * j] = p0[j], u.v[2 * j + 1] = p1[j];
-      *reinterpret_cast<Pack<T, 2 * P> *>(yv + first) = u;
+      put(yv + first, u);
     }
   }
 }
@@ -440,10 +477,6 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 // ---------------------------------------------------------------------------
 // Launch rules
 // ---------------------------------------------------------------------------
-
-bool vector_rows(const void *p, int64_t pitch, int esize) {
-  return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch * esize % 16 == 0);
-}
 
 constexpr int kNormBlocks = 1024;  // four workgroups of four waves on each of 256 CUs
 
@@ -458,19 +491,14 @@ bool pick_shape(int c, F &&f) {
     f(integral_constant<int, (L)>{}, integral_constant<int, (N)>{});                  \
     return true;                                                                      \
   }
-  if constexpr (V > 1) {
-    RT3D_SHAPE(8, 1)
-    RT3D_SHAPE(16, 1)
-    RT3D_SHAPE(32, 1)
-    RT3D_SHAPE(64, 1)
-    RT3D_SHAPE(64, 2)
-    RT3D_SHAPE(64, 4)
-    RT3D_SHAPE(256, 2)
-    RT3D_SHAPE(256, 4)
-  } else {
-    RT3D_SHAPE(64, 4)
-    RT3D_SHAPE(256, 4)
-  }
+  RT3D_SHAPE(8, 1)
+  RT3D_SHAPE(16, 1)
+  RT3D_SHAPE(32, 1)
+  RT3D_SHAPE(64, 1)
+  RT3D_SHAPE(64, 2)
+  RT3D_SHAPE(64, 4)
+  RT3D_SHAPE(256, 2)
+  RT3D_SHAPE(256, 4)
 #undef RT3D_SHAPE
   return false;
 }
@@ -536,22 +564,17 @@ int layernorm_bwd_blocks(int64_t rows, int c) {
 
 int launch_layernorm_fwd(const NormArgs &a, int dtype, void *stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int es = dtype == RT3D_F32 ? 4 : 2;
-  const bool vec = vector_rows(a.x, a.x_pitch, es) && vector_rows(a.y, a.y_pitch, es);
-  if (dtype == RT3D_F32) vec ? norm_fwd<float, 4>(a, s) : norm_fwd<float, 1>(a, s);
-  else if (dtype == RT3D_BF16) vec ? norm_fwd<__bf16, 8>(a, s) : norm_fwd<__bf16, 1>(a, s);
-  else vec ? norm_fwd<_Float16, 8>(a, s) : norm_fwd<_Float16, 1>(a, s);
+  if (dtype == RT3D_F32) norm_fwd<float, 4>(a, s);
+  else if (dtype == RT3D_BF16) norm_fwd<__bf16, 8>(a, s);
+  else norm_fwd<_Float16, 8>(a, s);
   return hipGetLastError();
 }
 
 int launch_layernorm_bwd(const NormArgs &a, int dtype, void *stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int es = dtype == RT3D_F32 ? 4 : 2;
-  const bool vec = vector_rows(a.x, a.x_pitch, es) && vector_rows(a.dy, a.y_pitch, es) &&
-                   vector_rows(a.dx, a.x_pitch, es);
-  if (dtype == RT3D_F32) vec ? norm_bwd<float, 4>(a, s) : norm_bwd<float, 1>(a, s);
-  else if (dtype == RT3D_BF16) vec ? norm_bwd<__bf16, 8>(a, s) : norm_bwd<__bf16, 1>(a, s);
-  else vec ? norm_bwd<_Float16, 8>(a, s) : norm_bwd<_Float16, 1>(a, s);
+  if (dtype == RT3D_F32) norm_bwd<float, 4>(a, s);
+  else if (dtype == RT3D_BF16) norm_bwd<__bf16, 8>(a, s);
+  else norm_bwd<_Float16, 8>(a, s);
   if (a.partial)
     layernorm_finalize_kernel<<<(2 * a.c + kFinalCols - 1) / kFinalCols, 256, 0, s>>>(a);
   return hipGetLastError();

@@ -364,18 +364,14 @@ rt3d_status rt3d_rope3d(const rt3d_rope_desc *d, const void *x, const int32_t *p
   a.t0 = d->t0;
   a.inverse = d->flags & RT3D_ROPE_INVERSE ? 1 : 0;
   const int halves = d->flags & RT3D_ROPE_HALVES ? 1 : 0;
-  // The widest access (16 bytes at most) that every run of a thread allows.
+  // The widest access (16 bytes at most) whose runs end with the vector (and the sections' halves).
   int pairs = halves ? 16 / es : 8 / es;
   const int rest = d->d - d->dt - d->dh - d->dw;
   auto fits = [&](int p) {
-    const int run = halves ? p : 2 * p;  // elements of an access
-    if (d->d % run || a.x_pitch % run || a.y_pitch % run || a.x_batch % run || a.y_batch % run) return false;
-    if (!aligned(x, run * es) || !aligned(y, run * es)) return false;
     if (!halves) return d->d % (2 * p) == 0;
     return d->dt / 2 % p == 0 && d->dh / 2 % p == 0 && d->dw / 2 % p == 0 && rest / 2 % p == 0;
   };
-  while (pairs > 1 && !fits(pairs)) pairs /= 2;
-  if (!fits(pairs)) return fail(RT3D_ERR_UNSUPPORTED, "pairs of neighbours need strides of whole pairs");
+  while (!fits(pairs)) pairs /= 2;  // one pair always fits: d and the sections are even
   a.slots = d->d / 2 / pairs;
   const int64_t base = static_cast<int64_t>(d->n) * a.tokens * a.slots;
   constexpr int64_t kThreads = 512 * 1024;  // two waves of threads for every SIMD's eight
