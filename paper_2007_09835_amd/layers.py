@@ -124,7 +124,7 @@ def _need(t: Optional[torch.Tensor], name: str, like: torch.Tensor, shape, dtype
         raise ValueError("%s is on %s, not on %s" % (name, t.device, like.device))
     if t.dtype != dtype:
         raise ValueError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:  # a torch.Size is a tuple
         raise ValueError("%s must be %s, not %s" % (name, list(shape), list(t.shape)))
 
 
@@ -137,7 +137,7 @@ def _launch(x: torch.Tensor, stream, call):
             raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, x.device))
         with torch.cuda.stream(stream):
             return call()
-    if x.device.index != torch.cuda.current_device():
+    if x.get_device() != torch._C._cuda_getDevice():
         with torch.cuda.device(x.device):
             return call()
     return call()
@@ -209,7 +209,9 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch
 
 def _rows_of(x: torch.Tensor, width: int, name: str):
     """(pitch, batch) of a [n, tokens, ...] tensor whose tokens hold ``width``
-    dense elements."""
+    dense elements; None where it is tight."""
+    if x.is_contiguous():
+        return None
     inner = 1
     for size, step in zip(reversed(x.shape[2:]), reversed(x.stride()[2:])):
         if size != 1 and step != inner:

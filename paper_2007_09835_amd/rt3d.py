@@ -226,7 +226,8 @@ def _dev_ptr(t, name: str) -> Optional[int]:
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        # the current device's current stream, without making a Stream object of it
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -381,7 +382,7 @@ def _view_ptr(t, name: str) -> Optional[int]:
         return None
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
-    if t.numel() and t.stride(-1) != 1 and t.shape[-1] != 1:
+    if not t.is_contiguous() and t.stride(-1) != 1 and t.shape[-1] != 1:
         raise ValueError("%s must be dense along its last dimension" % name)
     return t.data_ptr()
 
@@ -421,11 +422,19 @@ def rt3d_layernorm_bwd(desc: NormDesc, x, dy, gamma, mean, rstd, dx=None, dgamma
 
 
 def make_rope_desc(n, grid, vecs, d, sections, dtype="bf16", base=10000.0, t0=0, halves=False,
-                   inverse=False, x=(0, 0), y=(0, 0)) -> RopeDesc:
-    """Fill an rt3d_rope_desc (``x``, ``y``: (pitch, batch) of their rows)."""
+                   inverse=False, x=None, y=None) -> RopeDesc:
+    """Fill an rt3d_rope_desc (``x``, ``y``: (pitch, batch) of their rows, tight
+    where None)."""
     flags = (RT3D_ROPE_HALVES if halves else 0) | (RT3D_ROPE_INVERSE if inverse else 0)
-    return RopeDesc(n, *grid, vecs, d, *sections, t0, base, DTYPE_CODES[dtype], flags, Rows(*x),
-                    Rows(*y))
+    desc = RopeDesc(n, *grid, vecs, d, *sections, t0, base, DTYPE_CODES[dtype], flags)
+    _set_rows(desc, {"x": x, "y": y})
+    return desc
+
+
+def _set_rows(desc, rows) -> None:
+    for name, layout in rows.items():
+        if layout is not None:
+            setattr(desc, name, Rows(*layout))
 
 
 def rt3d_rope3d(desc: RopeDesc, x, pos, y, stream=None) -> None:
@@ -435,10 +444,10 @@ def rt3d_rope3d(desc: RopeDesc, x, pos, y, stream=None) -> None:
 
 def make_diffattn_desc(n, lq, lk, hq, hk, d, dtype="bf16", frame=0, scale=0.0, **rows) -> DiffAttnDesc:
     """Fill an rt3d_diffattn_desc; ``rows``: (pitch, batch) by tensor (q, o, k,
-    v, d_o, dq, dk, dv), tight where absent."""
-    return DiffAttnDesc(n, lq, lk, hq, hk, d, DTYPE_CODES[dtype], frame, scale,
-                        *(Rows(*rows.get(name, (0, 0)))
-                          for name in ("q", "o", "k", "v", "d_o", "dq", "dk", "dv")))
+    v, d_o, dq, dk, dv), tight where absent or None."""
+    desc = DiffAttnDesc(n, lq, lk, hq, hk, d, DTYPE_CODES[dtype], frame, scale)
+    _set_rows(desc, rows)
+    return desc
 
 
 def rt3d_diffattn_fwd_workspace_size(desc: DiffAttnDesc) -> int:
