@@ -103,14 +103,20 @@ struct Tile {
     return ((row & 3) << 2) | ((row >> 2) & 3);
   }
 
+  // A thread's next load lies kStep rows on; where that is a multiple of 16 its
+  // block is the same one, and one offset serves for all.
+  static constexpr int kStep = THREADS / kBlocks;
+  static constexpr int kOffsets = kStep % 16 == 0 ? 1 : kLoads;
+  using Offsets = unsigned[kOffsets];
+
   // Byte offsets of a thread's loads from the tile's first row in memory, or
   // far out of any tile where the block is padding (d < D).  SPLIT: a row is two
   // vectors of d padded to D each (queries, keys), else one of 2 d (values).
   template <bool SPLIT>
-  static __device__ __forceinline__ void offsets(int d, int64_t pitch, unsigned (&off)[kLoads]) {
+  static __device__ __forceinline__ void offsets(int d, int64_t pitch, Offsets &off) {
     constexpr int kPer = 16 / kEs;  // values of a block
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
+    for (int i = 0; i < kOffsets; ++i) {
       const int c = i * THREADS + static_cast<int>(threadIdx.x);
       const int row = c / kBlocks, blk = (c % kBlocks) ^ swizzle(row);
       int col = blk * kPer;
@@ -129,69 +135,81 @@ struct Tile {
   // Starts the loads of `rows` (0..ROWS) rows from `first` on; the other rows
   // of the tile become zeros.
   static __device__ __forceinline__ void stage(const T *first, int rows, int d, int64_t pitch,
-                                               const unsigned (&off)[kLoads], lds_char *to) {
+                                               const Offsets &off, lds_char *to) {
     const int bytes = rows > 0 ? static_cast<int>(((rows - 1) * pitch + 2 * d) * kEs) : 0;
     const __amdgpu_buffer_rsrc_t r =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(first), 0, bytes, 0x00020000);
     const int wave = uniform(static_cast<int>(threadIdx.x) >> 6);
+    const unsigned step = kOffsets == 1 ? static_cast<unsigned>(kStep * pitch * kEs) : 0;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           r, (__attribute__((address_space(3))) void *)(to + (i * THREADS + wave * 64) * 16), 16,
-          static_cast<int>(off[i]), 0, 0, 0);
+          static_cast<int>(off[kOffsets == 1 ? 0 : i] + i * step), 0, 0, 0);
   }
 
-  // Operand along the row: eight values from column `col` + 8 half of row `row`.
-  // col is a multiple of 16 and a constant; row0 + lane % 32.
-  static __device__ __forceinline__ Frag<T> along(const lds_char *t, int row0, int col) {
-    const int lane = threadIdx.x & 63, row = row0 + (lane & 31), f = swizzle(lane & 31);
-    const int half = lane >> 5;
+  // A lane's address of block 0 of its first row, for both kinds of reads; a
+  // block's number only changes bits 4 to 7 of it, by an XOR (tiles begin at
+  // multiples of 256 bytes), and rows and blocks beyond those are offsets of the
+  // read itself.  `at` adds a tile to it, out of the compiler's sight: it would
+  // keep one register for every block otherwise.
+  static __device__ __forceinline__ unsigned lane_along() {
+    const int lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
+    return row * kRowBytes + (((kEs == 2 ? half : 2 * half) ^ swizzle(row)) << 4);
+  }
+  static __device__ __forceinline__ unsigned lane_across() {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
     if constexpr (kEs == 2) {
-      const int blk = col / 8, at = (blk & ~15) + (((blk & 15) | half) ^ f);
-      return *reinterpret_cast<const __attribute__((address_space(3))) Frag<T> *>(t + row * kRowBytes + at * 16);
+      // the transposing read: in 16 lanes, lane 4 r + c reads four values of row
+      // r, and receives those of its own column from four rows
+      const int row = 4 * half + ((lane & 15) >> 2), sub = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      return row * kRowBytes + ((sub ^ swizzle(row)) << 4) + (lane & 1) * 8;
     } else {
-      const int blk = col / 4, at = (blk & ~15);
-      const auto *p = t + row * kRowBytes + at * 16;
-      const auto a = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(
-          p + ((((blk & 15) | (2 * half)) ^ f) * 16));
-      const auto b = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(
-          p + ((((blk & 15) | (2 * half) | 1) ^ f) * 16));
-      return Frag<T>{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      return 4 * half * kRowBytes + ((((lane & 31) >> 2) ^ half) << 4) + (lane & 3) * 4;
     }
+  }
+  static __device__ __forceinline__ unsigned at(unsigned lane, const lds_char *tile) {
+    unsigned v = lane + static_cast<unsigned>(reinterpret_cast<uintptr_t>(tile));
+    asm volatile("" : "+v"(v));
+    return v;
+  }
+  template <typename V>
+  static __device__ __forceinline__ V read(unsigned base, int blk, int rows) {
+    return *(const __attribute__((address_space(3))) V *)static_cast<uintptr_t>(
+        (base ^ ((blk & 15) << 4)) + (blk & ~15) * 16 + rows * kRowBytes);
+  }
+
+  // Operand along the row: eight values from column `col` + 8 half of row row0 +
+  // lane % 32 (row0, col: constants, multiples of 32 and 16).
+  static __device__ __forceinline__ Frag<T> along(unsigned base, int row0, int col) {
+    if constexpr (kEs == 2) return read<Frag<T>>(base, col / 8, row0);
+    const auto a = read<f32x4>(base, col / 4, row0), b = read<f32x4>(base, col / 4 + 1, row0);
+    return Frag<T>{static_cast<T>(a[0]), static_cast<T>(a[1]), static_cast<T>(a[2]), static_cast<T>(a[3]),
+                   static_cast<T>(b[0]), static_cast<T>(b[1]), static_cast<T>(b[2]), static_cast<T>(b[3])};
   }
 
   // Transposed operand: column `col` + lane % 32, and of the 16 rows from row0
   // on those that a result's registers hold for the half: value e is row
   // row0 + 8 (e / 4) + 4 half + e % 4.  row0 and col: multiples of 16 and 32.
-  static __device__ __forceinline__ Frag<T> across(const lds_char *t, int row0, int col) {
-    const int lane = threadIdx.x & 63, half = lane >> 5;
+  static __device__ __forceinline__ Frag<T> across(unsigned base, int row0, int col) {
     if constexpr (kEs == 2) {
-      // the transposing read: in 16 lanes, lane 4 r + c reads four values of row
-      // r, and receives those of its own column from four rows
-      const int r = (lane & 15) >> 2;
-      const int sub = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
       union {
         s16x4 half4[2];
         Frag<T> all;
       } u;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int row = row0 + 8 * j + 4 * half + r, blk = col / 8;
-        const int at = (blk & ~15) + (((blk & 15) | sub) ^ swizzle(row));
+        const int blk = (col / 8) ^ (2 * j);  // rows 8 further on: their swizzle differs by 2
         u.half4[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4 *)(t + row * kRowBytes + at * 16 + (lane & 1) * 8));
+            (__attribute__((address_space(3))) s16x4 *)static_cast<uintptr_t>(
+                (base ^ ((blk & 15) << 4)) + (blk & ~15) * 16 + (row0 + 8 * j) * kRowBytes));
       }
       return u.all;
     } else {
       Frag<T> v;
-      const int c = col + (lane & 31);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int row = row0 + 8 * (e / 4) + 4 * half + e % 4, blk = c / 4;
-        const int at = (blk & ~15) + ((blk & 15) ^ swizzle(row));
-        v[e] = *reinterpret_cast<const __attribute__((address_space(3))) float *>(
-            t + row * kRowBytes + at * 16 + (c & 3) * 4);
-      }
+      for (int e = 0; e < 8; ++e)
+        v[e] = read<T>(base, (col / 4) ^ ((e % 4) << 2 | 2 * (e / 4)), row0 + 8 * (e / 4) + e % 4);
       return v;
     }
   }

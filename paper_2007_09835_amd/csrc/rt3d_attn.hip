@@ -30,6 +30,11 @@ struct Fwd {
   using KV = Tile<T, D, kKeys, kThreads>;
   static constexpr int kLds = 4 * KV::kBytes;
   static constexpr int kMinWaves = sizeof(T) == 2 ? 2 : 1;
+  // operands read ahead of their products: registers for them are left in 16 bits
+  static constexpr bool kAhead = sizeof(T) == 2;
+  // The transposing reads wait for every load under way: the next tile's loads
+  // start behind the first ones of a tile that has more, else at once.
+  static constexpr bool kLate = kKeys == 64;
   static_assert(kMaps == 2 || ROWS * 32 * kWidth * 4 <= kLds, "the second maps' results fit");
 };
 
@@ -42,7 +47,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
     AttnArgs a) {
   using F = Fwd<T, D, ROWS>;
   using KV = typename F::KV;
-  constexpr int kKeys = F::kKeys, kSub = kKeys / 32, kTiles = F::kWidth / 32, kMaps = F::kMaps;
+  constexpr int kKeys = F::kKeys, kTiles = F::kWidth / 32, kMaps = F::kMaps;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char *lds = (lds_char *)smem;
 
@@ -91,7 +96,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
           q[m][s] = in && col < a.d ? load_frag(p + m * a.d + col) : Frag<T>{};
         }
     }
-    unsigned k_off[KV::kLoads], v_off[KV::kLoads];
+    typename KV::Offsets k_off, v_off;
     KV::template offsets<true>(a.d, a.k_pitch, k_off);
     KV::template offsets<false>(a.d, a.v_pitch, v_off);
     const T *k = static_cast<const T *>(a.k) + clip * a.k_batch + static_cast<int64_t>(kvh) * 2 * a.d;
@@ -101,68 +106,111 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
       KV::stage(k + key * a.k_pitch, n, a.d, a.k_pitch, k_off, lds + buf * 2 * KV::kBytes);
       KV::stage(v + key * a.v_pitch, n, a.d, a.v_pitch, v_off, lds + (buf * 2 + 1) * KV::kBytes);
     };
+    // (a second map's vectors begin a whole number of 16 blocks on: beyond d = 64)
+    const unsigned k_lane = KV::lane_along() + map0 * D * KV::kEs, v_lane = KV::lane_across();
     stage(begin, 0);
     int buf = 0;
-    for (int key = begin; key < end; key += kKeys, buf ^= 1) {
+    for (int tile_key = begin; tile_key < end; tile_key += kKeys, buf ^= 1) {
       tile_barrier();  // this tile has landed, and the other buffer is read
-      if (key + kKeys < end) stage(key + kKeys, buf ^ 1);
-      if (key >= wave_end) continue;
-      const lds_char *kt = lds + buf * 2 * KV::kBytes, *vt = kt + KV::kBytes;
-      const bool masked = key + kKeys > whole;
-      Frag<T> p[kMaps][2 * kSub];
+      const unsigned kt = KV::at(k_lane, lds + buf * 2 * KV::kBytes), vt = KV::at(v_lane, lds + (buf * 2 + 1) * KV::kBytes);
+      const bool more = tile_key + kKeys < end;
+      if (!F::kLate && more) stage(tile_key + kKeys, buf ^ 1);
 #pragma unroll
-      for (int m = 0; m < kMaps; ++m) {
-        f32x16 s[kSub] = {};
+      for (int j = 0; j < kKeys; j += 32) {
+        const int key = tile_key + j;
+        if (key >= wave_end) {
+          if (F::kLate && j == 0 && more) stage(tile_key + kKeys, buf ^ 1);
+          break;
+        }
+        f32x16 s[kMaps] = {};
+        if constexpr (F::kAhead) {
+          // keys' operands, D / 16 products ahead of their use
+          constexpr int kN = kMaps * D / 16, kRing = D / 16 < 4 ? D / 16 : 4;
+          Frag<T> f[kRing];
 #pragma unroll
-        for (int j = 0; j < kSub; ++j)
+          for (int i = 0; i < kRing; ++i) f[i] = KV::along(kt, j, i * 16);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i)
-            s[j] = Mma<T>::run(KV::along(kt + map0 * D * KV::kEs, j * 32, m * D + i * 16), q[m][i], s[j]);
-        if (masked) {
+          for (int i = 0; i < kN; ++i) {
+            const int m = i / (D / 16);
+            s[m] = Mma<T>::run(f[i % kRing], q[m][i % (D / 16)], s[m]);
+            if (i + kRing < kN) f[i % kRing] = KV::along(kt, j, (i + kRing) * 16);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        } else {
 #pragma unroll
-          for (int j = 0; j < kSub; ++j)
+          for (int m = 0; m < kMaps; ++m)
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) s[m] = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s[m]);
+        }
+        Frag<T> v0[kTiles];  // values of the first 16 keys, on their way during the softmax
+        if constexpr (F::kAhead) {
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) v0[t] = KV::across(vt, j, t * 32);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (F::kLate && j == 0 && more) stage(tile_key + kKeys, buf ^ 1);
+        if (key + 32 > whole) {
+#pragma unroll
+          for (int m = 0; m < kMaps; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (key + j * 32 + result_row(i, half) >= limit) s[j][i] = -INFINITY;
+              if (key + result_row(i, half) >= limit) s[m][i] = -INFINITY;
         }
-        float most = s[0][0];
+        float most[kMaps];
+        bool up = false;
 #pragma unroll
-        for (int j = 0; j < kSub; ++j)
+        for (int m = 0; m < kMaps; ++m) {
+          most[m] = s[m][0];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) most = fmaxf(most, s[j][i]);
-        most = half_max(most) * a.scale2;
-        if (__any(most > top[m] + kSlack)) {
-          const float now = fmaxf(top[m], most);
-          const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
-          top[m] = now;
-          sum[m] *= by;
-#pragma unroll
-          for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[m][t][i] *= by;
+          for (int i = 1; i < 16; ++i) most[m] = fmaxf(most[m], s[m][i]);
+          most[m] = half_max(most[m]) * a.scale2;
+          up |= most[m] > top[m] + kSlack;
         }
-        const float ref = top[m] == -INFINITY ? 0.f : -top[m];
+        if (__any(up)) {
 #pragma unroll
-        for (int j = 0; j < kSub; ++j) {
+          for (int m = 0; m < kMaps; ++m) {
+            const float now = fmaxf(top[m], most[m]);
+            const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
+            top[m] = now;
+            sum[m] *= by;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[m][t][i] *= by;
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < kMaps; ++m) {
+          const float ref = top[m] == -INFINITY ? 0.f : -top[m];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            s[j][i] = __builtin_amdgcn_exp2f(fmaf(s[j][i], a.scale2, ref));
-            sum[m] += s[j][i];
+            s[m][i] = __builtin_amdgcn_exp2f(fmaf(s[m][i], a.scale2, ref));
+            sum[m] += s[m][i];
           }
-          // Rounded to the layer's type for the product with v (half a step of
-          // each probability); their sum keeps 32 bits.
-          p[m][2 * j] = pack<T>(s[j], 0);
-          p[m][2 * j + 1] = pack<T>(s[j], 8);
         }
+        // Rounded to the layer's type for the product with v (half a step of
+        // each probability); their sums keep 32 bits.
+        Frag<T> p[kMaps][2];
+#pragma unroll
+        for (int m = 0; m < kMaps; ++m) p[m][0] = pack<T>(s[m], 0), p[m][1] = pack<T>(s[m], 8);
+        Frag<T> v1[kTiles];
+        if constexpr (F::kAhead) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) v1[t] = KV::across(vt, j + 16, t * 32);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            Frag<T> f;
+            if constexpr (F::kAhead) f = h ? v1[t] : v0[t];
+            else f = KV::across(vt, j + 16 * h, t * 32);
+#pragma unroll
+            for (int m = 0; m < kMaps; ++m) acc[m][t] = Mma<T>::run(f, p[m][h], acc[m][t]);
+          }
       }
-#pragma unroll
-      for (int s = 0; s < 2 * kSub; ++s)
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          const Frag<T> f = KV::across(vt, s * 16, t * 32);
-#pragma unroll
-          for (int m = 0; m < kMaps; ++m) acc[m][t] = Mma<T>::run(f, p[m][s], acc[m][t]);
-        }
     }
   }
 

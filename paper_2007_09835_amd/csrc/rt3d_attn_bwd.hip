@@ -103,7 +103,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
         }
       }
     }
-    unsigned k_off[KV::kLoads], v_off[KV::kLoads];
+    typename KV::Offsets k_off, v_off;
     KV::template offsets<true>(a.d, a.k_pitch, k_off);
     KV::template offsets<false>(a.d, a.v_pitch, v_off);
     const T *k = static_cast<const T *>(a.k) + clip * a.k_batch + static_cast<int64_t>(kvh) * 2 * a.d;
@@ -113,14 +113,17 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       KV::stage(k + key * a.k_pitch, n, a.d, a.k_pitch, k_off, lds + buf * 2 * KV::kBytes);
       KV::stage(v + key * a.v_pitch, n, a.d, a.v_pitch, v_off, lds + (buf * 2 + 1) * KV::kBytes);
     };
+    const unsigned along = KV::lane_along(), across = KV::lane_across();
     stage(begin, 0);
     int buf = 0;
     for (int key = begin; key < end; key += kKeys, buf ^= 1) {
       tile_barrier();
       if (key + kKeys < end) stage(key + kKeys, buf ^ 1);
       if (key >= wave_end) continue;
-      const lds_char *kt = lds + buf * 2 * KV::kBytes, *vt = kt + KV::kBytes;
+      const lds_char *tile_k = lds + buf * 2 * KV::kBytes;
+      const unsigned kt = KV::at(along, tile_k), vt = KV::at(along, tile_k + KV::kBytes), kc = KV::at(across, tile_k);
       const bool masked = key + kKeys > whole;
+#pragma unroll
       for (int j = 0; j < kKeys; j += 32) {
         f32x16 dp = {};
 #pragma unroll
@@ -148,8 +151,8 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
           const Frag<T> lo = pack<T>(s, 0), hi = pack<T>(s, 8);
 #pragma unroll
           for (int t = 0; t < D / 32; ++t) {
-            acc[m][t] = Mma<T>::run(KV::across(kt, j, m * D + t * 32), lo, acc[m][t]);
-            acc[m][t] = Mma<T>::run(KV::across(kt, j + 16, m * D + t * 32), hi, acc[m][t]);
+            acc[m][t] = Mma<T>::run(KV::across(kc, j, m * D + t * 32), lo, acc[m][t]);
+            acc[m][t] = Mma<T>::run(KV::across(kc, j + 16, m * D + t * 32), hi, acc[m][t]);
           }
         }
       }
@@ -283,13 +286,13 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
     }
     lds_char *keys = lds + 2 * F::kBuffer;
     if constexpr (F::kLdsK) {
-      unsigned k_off[F::K::kLoads];
+      typename F::K::Offsets k_off;
       F::K::template offsets<true>(a.d, a.k_pitch, k_off);
       F::K::stage(static_cast<const T *>(a.k) + clip * a.k_batch + key_block * a.k_pitch +
                       static_cast<int64_t>(kvh) * 2 * a.d,
                   min(32 * WAVES, k_len - key_block), a.d, a.k_pitch, k_off, keys);
     }
-    unsigned q_off[Q::kLoads], g_off[Q::kLoads];
+    typename Q::Offsets q_off, g_off;
     Q::template offsets<true>(a.d, a.q_pitch, q_off);
     Q::template offsets<false>(a.d, a.do_pitch, g_off);
     const int64_t map = static_cast<int64_t>(a.n) * a.hq * a.lq;
@@ -320,6 +323,9 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
         ++st_head;
       }
     };
+    const unsigned along = Q::lane_along(), across = Q::lane_across();
+    unsigned key_lane = 0;
+    if constexpr (F::kLdsK) key_lane = F::K::lane_along() + wave * 32 * F::K::kRowBytes;
     stage(0);
     int buf = 0;
     for (int t = from_tile; t < to_tile; ++t, buf ^= 1) {
@@ -333,7 +339,11 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       }
       // no row of the tile sees a key of this wave, or it has none
       if (at + kRows <= from_wave || key_wave >= k_len) continue;
-      const lds_char *qt = lds + buf * F::kBuffer, *gt = qt + Q::kBytes, *st = gt + Q::kBytes;
+      const lds_char *tile_q = lds + buf * F::kBuffer, *tile_g = tile_q + Q::kBytes, *st = tile_g + Q::kBytes;
+      const unsigned qt = Q::at(along, tile_q), gt = Q::at(along, tile_g);
+      const unsigned qc = Q::at(across, tile_q), gc = Q::at(across, tile_g);
+      unsigned kt = 0;
+      if constexpr (F::kLdsK) kt = F::K::at(key_lane, keys);
       // some pair of the tile is masked, or some row has a single key
       const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
       const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
@@ -353,7 +363,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
         for (int i = 0; i < D / 16; ++i) {
           Frag<T> b;
           if constexpr (F::kHoldK) b = kf[m][i];
-          else if constexpr (F::kLdsK) b = F::K::along(keys, wave * 32, m * D + i * 16);
+          else if constexpr (F::kLdsK) b = F::K::along(kt, 0, m * D + i * 16);
           else b = key_frag(m, i);
           s = Mma<T>::run(Q::along(qt, 0, m * D + i * 16), b, s);
         }
@@ -388,7 +398,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
           const Frag<T> ds = pack<T>(s, 8 * h);
 #pragma unroll
           for (int c = 0; c < D / 32; ++c)
-            dk[m][c] = Mma<T>::run(Q::across(qt, 16 * h, m * D + c * 32), ds, dk[m][c]);
+            dk[m][c] = Mma<T>::run(Q::across(qc, 16 * h, m * D + c * 32), ds, dk[m][c]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -396,7 +406,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       for (int h = 0; h < 2; ++h) {
         const Frag<T> p = pack<T>(pv, 8 * h);
 #pragma unroll
-        for (int c = 0; c < 2 * D / 32; ++c) dv[c] = Mma<T>::run(Q::across(gt, 16 * h, c * 32), p, dv[c]);
+        for (int c = 0; c < 2 * D / 32; ++c) dv[c] = Mma<T>::run(Q::across(gc, 16 * h, c * 32), p, dv[c]);
       }
     }
   }
