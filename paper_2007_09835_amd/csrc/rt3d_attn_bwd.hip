@@ -22,6 +22,9 @@ struct Dq {
   using KV = Tile<T, D, kKeys, kThreads>;
   static constexpr int kLds = 4 * KV::kBytes;
   static constexpr int kMinWaves = sizeof(T) == 2 && D <= 64 ? 2 : 1;
+  // 32-bit output gradients of 256 columns beside the queries pass the register
+  // file: they are read again for every step, from L1.
+  static constexpr bool kHoldG = sizeof(T) == 2 || D <= 64;
 };
 
 // Rows of queries as in the forward pass (a lane holds a row): S^T = K Q^T and
@@ -62,8 +65,14 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   float dl = 0.f;
 
   if (begin < end) {
-    Frag<T> q[2][D / 16], g[2 * D / 16];
+    Frag<T> q[2][D / 16], g[F::kHoldG ? 2 * D / 16 : 1];
     float lse[2] = {INFINITY, INFINITY}, mean[2] = {0.f, 0.f};
+    const T *go = static_cast<const T *>(a.d_o) + clip * a.do_batch + query * a.do_pitch +
+                  static_cast<int64_t>(head) * 2 * a.d;
+    auto grad_frag = [&](int s) {
+      const int col = s * 16 + 8 * half;
+      return in && col < 2 * a.d ? load_frag(go + col) : Frag<T>{};
+    };
     {
       const T *p = static_cast<const T *>(a.q) + clip * a.q_batch + query * a.q_pitch +
                    static_cast<int64_t>(head) * 2 * a.d;
@@ -74,8 +83,6 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
           const int col = s * 16 + 8 * half;
           q[m][s] = in && col < a.d ? load_frag(p + m * a.d + col) : Frag<T>{};
         }
-      const T *go = static_cast<const T *>(a.d_o) + clip * a.do_batch + query * a.do_pitch +
-                    static_cast<int64_t>(head) * 2 * a.d;
       const T *o = static_cast<const T *>(a.o) + clip * a.o_batch + query * a.o_pitch +
                    static_cast<int64_t>(head) * 2 * a.d;
       const T *o2 = static_cast<const T *>(a.o2) +
@@ -84,12 +91,13 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       for (int s = 0; s < 2 * D / 16; ++s) {
         const int col = s * 16 + 8 * half;
         const bool get = in && col < 2 * a.d;
-        g[s] = get ? load_frag(go + col) : Frag<T>{};
+        const Frag<T> grad = grad_frag(s);
+        if constexpr (F::kHoldG) g[s] = grad;
         const Frag<T> x = get ? load_frag(o + col) : Frag<T>{}, y = get ? load_frag(o2 + col) : Frag<T>{};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          mean[0] += static_cast<float>(g[s][e]) * static_cast<float>(x[e]);
-          mean[1] += static_cast<float>(g[s][e]) * static_cast<float>(y[e]);
+          mean[0] += static_cast<float>(grad[e]) * static_cast<float>(x[e]);
+          mean[1] += static_cast<float>(grad[e]) * static_cast<float>(y[e]);
         }
       }
       mean[1] = half_sum(mean[1]);
@@ -127,7 +135,12 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       for (int j = 0; j < kKeys; j += 32) {
         f32x16 dp = {};
 #pragma unroll
-        for (int i = 0; i < 2 * D / 16; ++i) dp = Mma<T>::run(KV::along(vt, j, i * 16), g[i], dp);
+        for (int i = 0; i < 2 * D / 16; ++i) {
+          Frag<T> b;
+          if constexpr (F::kHoldG) b = g[i];
+          else b = grad_frag(i);
+          dp = Mma<T>::run(KV::along(vt, j, i * 16), b, dp);
+        }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
           f32x16 s = {};
@@ -218,14 +231,18 @@ struct Dkv {
   // otherwise keys wait in LDS.  32-bit values of 256 columns (and their keys)
   // pass both: they are read again for every tile, from L1.
   static constexpr bool kHoldV = sizeof(T) == 2 || D <= 64, kHoldK = D <= 32, kLdsK = !kHoldK && kHoldV;
+  // Beyond d = 64 both gradients (2 x 32 x 256 results) would take every
+  // accumulator and leave none for scores: the kernel runs once for each.
+  static constexpr bool kApart = D > 64;
   using K = Tile<T, D, 32 * WAVES, kThreads>;
   static constexpr int kBuffer = 2 * Q::kBytes + kStat;
   static constexpr int kLds = 2 * kBuffer + (kLdsK ? K::kBytes : 0);
 };
 
 // SPLIT: the query tiles of a key head (its group's heads, one after another) are
-// split over workgroups, which leave 32-bit partial gradients.
-template <typename T, int D, int WAVES, bool SPLIT>
+// split over workgroups, which leave 32-bit partial gradients.  DK, DV: which
+// gradients this launch makes.
+template <typename T, int D, int WAVES, bool SPLIT, bool DK, bool DV>
 __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void attn_dkv_kernel(AttnArgs a) {
   using F = Dkv<T, D, WAVES>;
   using Q = typename F::Q;
@@ -252,7 +269,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
   const bool single_all = k_len == 1;
   const int single = a.frame == 1 ? q_len - k_len : -1;
 
-  f32x16 dk[2][D / 32] = {}, dv[2 * D / 32] = {};
+  f32x16 dk[2][DK ? D / 32 : 1] = {}, dv[DV ? 2 * D / 32 : 1] = {};
   const int begin = max(0, first_query(key_block)) / kRows * kRows;
 
   // query tiles that see the workgroup's keys, a group's heads after one another,
@@ -275,12 +292,12 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       const int col = s * 16 + 8 * half;
       return in && col < 2 * a.d ? load_frag(v + col) : Frag<T>{};
     };
-    Frag<T> kf[F::kHoldK ? 2 : 1][F::kHoldK ? D / 16 : 1], vf[F::kHoldV ? 2 * D / 16 : 1];
+    Frag<T> kf[F::kHoldK ? 2 : 1][F::kHoldK ? D / 16 : 1], vf[F::kHoldV && DK ? 2 * D / 16 : 1];
     if constexpr (F::kHoldK) {
 #pragma unroll
       for (int s = 0; s < D / 16; ++s) kf[0][s] = key_frag(0, s), kf[1][s] = key_frag(1, s);
     }
-    if constexpr (F::kHoldV) {
+    if constexpr (F::kHoldV && DK) {
 #pragma unroll
       for (int s = 0; s < 2 * D / 16; ++s) vf[s] = value_frag(s);
     }
@@ -348,12 +365,14 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
       const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
       f32x16 dp = {}, pv;
+      if constexpr (DK) {
 #pragma unroll
-      for (int i = 0; i < 2 * D / 16; ++i) {
-        Frag<T> b;
-        if constexpr (F::kHoldV) b = vf[i];
-        else b = value_frag(i);
-        dp = Mma<T>::run(Q::along(gt, 0, i * 16), b, dp);
+        for (int i = 0; i < 2 * D / 16; ++i) {
+          Frag<T> b;
+          if constexpr (F::kHoldV) b = vf[i];
+          else b = value_frag(i);
+          dp = Mma<T>::run(Q::along(gt, 0, i * 16), b, dp);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -384,10 +403,11 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
           for (int e = 0; e < 4; ++e) {
             const int i = 4 * r + e;
             const float p = by * __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -lse[e]));
-            pv[i] = m ? pv[i] + p : p;
+            if (DV) pv[i] = m ? pv[i] + p : p;
             s[i] = p * (dp[i] - mean[e]);
           }
         }
+        if constexpr (!DK) continue;
         if (lone) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -403,7 +423,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; DV && h < 2; ++h) {
         const Frag<T> p = pack<T>(pv, 8 * h);
 #pragma unroll
         for (int c = 0; c < 2 * D / 32; ++c) dv[c] = Mma<T>::run(Q::across(gc, 16 * h, c * 32), p, dv[c]);
@@ -415,7 +435,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
     float *p = a.part + ((split * static_cast<int64_t>(a.n) + clip) * a.lk + key) * a.hk * 4 * a.d +
                static_cast<int64_t>(kvh) * 4 * a.d;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; DK && m < 2; ++m)
 #pragma unroll
       for (int t = 0; t < D / 32; ++t)
 #pragma unroll
@@ -427,7 +447,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
                       dk[m][t][4 * r + 3] * a.scale};
         }
 #pragma unroll
-    for (int t = 0; t < 2 * D / 32; ++t)
+    for (int t = 0; DV && t < 2 * D / 32; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int col = t * 32 + 8 * r + 4 * half;
@@ -440,7 +460,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
   struct alignas(4 * sizeof(T)) Four {
     T v[4];
   };
-  if (a.dk) {
+  if (DK && a.dk) {
     T *p = static_cast<T *>(a.dk) + clip * a.dk_batch + key * a.dk_pitch + static_cast<int64_t>(kvh) * 2 * a.d;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -456,7 +476,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
           *reinterpret_cast<Four *>(p + m * a.d + col) = x;
         }
   }
-  if (a.dv) {
+  if (DV && a.dv) {
     T *p = static_cast<T *>(a.dv) + clip * a.dv_batch + key * a.dv_pitch + static_cast<int64_t>(kvh) * 2 * a.d;
 #pragma unroll
     for (int t = 0; t < 2 * D / 32; ++t)
@@ -560,18 +580,31 @@ int launch_dq(AttnArgs a, const BwdPlan &p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, int D, bool SPLIT>
-int launch_dkv(AttnArgs a, const BwdPlan &p, hipStream_t s) {
+template <typename T, int D, bool SPLIT, bool DK, bool DV>
+int launch_keys(const AttnArgs &a, hipStream_t s) {
   constexpr int kWaves = kBwdRows / 32;
   using F = Dkv<T, D, kWaves>;
-  const int e = allow_lds<attn_dkv_kernel<T, D, kWaves, SPLIT>>(F::kLds);
+  const int e = allow_lds<attn_dkv_kernel<T, D, kWaves, SPLIT, DK, DV>>(F::kLds);
   if (e != hipSuccess) return e;
+  attn_dkv_kernel<T, D, kWaves, SPLIT, DK, DV><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int D, bool SPLIT>
+int launch_dkv(AttnArgs a, const BwdPlan &p, hipStream_t s) {
   a.tiles = (a.lk + kBwdRows - 1) / kBwdRows;
   a.splits = p.dkv_splits;
   a.blocks = static_cast<int64_t>(a.n) * a.hk * a.tiles * a.splits;
   a.part = a.rowstat + p.dkv_part;
   if (a.blocks == 0) return hipSuccess;
-  attn_dkv_kernel<T, D, kWaves, SPLIT><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
+  int e = hipSuccess;
+  if constexpr (Dkv<T, D, kBwdRows / 32>::kApart) {
+    if (a.dk) e = launch_keys<T, D, SPLIT, true, false>(a, s);
+    if (e == hipSuccess && a.dv) e = launch_keys<T, D, SPLIT, false, true>(a, s);
+  } else {
+    e = launch_keys<T, D, SPLIT, true, true>(a, s);
+  }
+  if (e != hipSuccess) return e;
   if (SPLIT) {
     const int64_t threads = static_cast<int64_t>(a.n) * a.lk * a.hk * a.d;
     attn_sum_kernel<T, true><<<static_cast<unsigned>((threads + 255) / 256), 256, 0, s>>>(a);

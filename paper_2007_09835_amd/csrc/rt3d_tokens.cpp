@@ -181,14 +181,19 @@ AttnArgs attn_args(const rt3d_diffattn_desc *d, const Shape &s) {
 // without splits, each a walk of `steps` steps of `step_us` on a CU of its own;
 // part_bytes: one split's partial results, written and read once at 4 TB/s; a
 // split call pays 5 us for its second launch.  The time is that of the fullest
-// CU; more than one workgroup on a CU run at 0.6 of the sum of their times.
+// CU; workgroups that share one take `shared` of the sum of their times (16-bit
+// ones fill each other's waits, 32-bit ones wait for the same matrix units).
+// Two clips of 392 tokens in 32 bits: 7 splits of dq and dk/dv 31 and 36 us, 4
+// splits 26 and 31, none 56 and 70.
 constexpr int kCus = 256;
-int pick_splits(int64_t blocks, int64_t steps, double step_us, double part_bytes, int64_t most) {
+int pick_splits(const rt3d_diffattn_desc *d, int64_t blocks, int64_t steps, double step_us, double part_bytes,
+                int64_t most) {
   if (blocks <= 0 || blocks >= 2 * kCus || steps < 2) return 1;
+  const double shared = d->dtype == RT3D_F32 ? 1.0 : 0.6;
   auto time = [&](int64_t s) {
     const double on_cu = static_cast<double>((blocks * s + kCus - 1) / kCus);
     const double walk = static_cast<double>((steps + s - 1) / s) * step_us;
-    return walk * std::max(1.0, 0.6 * on_cu) + (s > 1 ? 5.0 + 2 * s * part_bytes / 4e6 : 0.0);
+    return walk * std::max(1.0, shared * on_cu) + (s > 1 ? 5.0 + 2 * s * part_bytes / 4e6 : 0.0);
   };
   int best = 1;
   for (int64_t s = 2; s <= most && s <= steps; ++s)
@@ -200,8 +205,8 @@ int pick_splits(int64_t blocks, int64_t steps, double step_us, double part_bytes
 int split_span(int lk, int splits) { return static_cast<int>((static_cast<int64_t>(lk) + splits - 1) / splits + 63) / 64 * 64; }
 
 // Time of a step of 32 keys (forward, dq) or 32 queries (dk, dv) of a workgroup
-// alone on its CU, in us per 32 channels of d: 16-bit products are issued in a
-// sixteenth of the time of 32-bit ones.
+// alone on its CU, in us per 32 channels of d: 32-bit steps take their products
+// (6144 or 8192 cycles of the matrix unit), 16-bit ones the rest as well.
 double step_us(const rt3d_diffattn_desc *d, double bits16, double bits32) {
   const int wide = d->d <= 32 ? 1 : d->d <= 64 ? 2 : 4;
   return wide * (d->dtype == RT3D_F32 ? bits32 : bits16);
@@ -232,7 +237,7 @@ FwdPlan fwd_plan(const rt3d_diffattn_desc *d, const Shape &s, uint64_t workspace
     // bound by the cache's bytes: enough waves to keep them coming
     splits = std::min<int64_t>({most, kSplitBlocks / p.blocks, d->lk / kSplitKeys});
   } else {
-    splits = pick_splits(p.blocks, (d->lk + 31) / 32, step_us(d, 0.35, 1.3), static_cast<double>(one), most);
+    splits = pick_splits(d, p.blocks, (d->lk + 31) / 32, step_us(d, 0.35, 2.9), static_cast<double>(one), most);
   }
   if (splits > 1) {
     p.span = split_span(d->lk, static_cast<int>(splits));
@@ -251,14 +256,14 @@ BwdPlan bwd_plan(const rt3d_diffattn_desc *d, const Shape &s) {
   const uint64_t stats = static_cast<uint64_t>(d->n) * d->hq * d->lq;
   const uint64_t dq = stats * 2 * d->d, dkv = static_cast<uint64_t>(pairs) * d->lk * 4 * d->d;
   p.dq_span = d->lk;
-  p.dq_splits = pick_splits(pairs * ((rows + kBwdRows - 1) / kBwdRows), (d->lk + 31) / 32,
-                            step_us(d, 0.35, 1.3), dq * 4.0, 16);
+  p.dq_splits = pick_splits(d, pairs * ((rows + kBwdRows - 1) / kBwdRows), (d->lk + 31) / 32,
+                            step_us(d, 0.35, 2.9), dq * 4.0, 16);
   if (p.dq_splits > 1) {
     p.dq_span = split_span(d->lk, p.dq_splits);
     p.dq_splits = (d->lk + p.dq_span - 1) / p.dq_span;
   }
-  p.dkv_splits = pick_splits(pairs * ((d->lk + kBwdRows - 1) / kBwdRows),
-                             static_cast<int64_t>(s.group) * ((d->lq + 31) / 32), step_us(d, 0.45, 1.8),
+  p.dkv_splits = pick_splits(d, pairs * ((d->lk + kBwdRows - 1) / kBwdRows),
+                             static_cast<int64_t>(s.group) * ((d->lq + 31) / 32), step_us(d, 0.45, 3.9),
                              dkv * 4.0, 16);
   auto up = [](uint64_t floats) { return (floats + 3) / 4 * 4; };  // parts begin at 16 bytes
   p.dq_part = up((2 + p.dq_splits) * stats);
