@@ -343,24 +343,26 @@ __global__ __launch_bounds__(kNormThreads) void layernorm_columns_kernel(NormArg
   out[a.c + col] = db;
 }
 
-// dgamma and dbeta: the workgroups' partial sums, 16 runs of them added in order
-// by 16 threads of a column, and then the runs.
-constexpr int kFinalCols = 16;
-__global__ __launch_bounds__(256) void layernorm_finalize_kernel(NormArgs a) {
-  __shared__ float lds[16][kFinalCols];
+// dgamma and dbeta: the workgroups' partial sums, kFinalRuns runs of them added in
+// order by as many threads of a column, and then the runs.
+constexpr int kFinalCols = 16, kFinalRuns = 64;
+__global__ __launch_bounds__(kFinalCols * kFinalRuns) void layernorm_finalize_kernel(NormArgs a) {
+  __shared__ float lds[kFinalRuns][kFinalCols];
   const int c2 = 2 * a.c;
   const int col = blockIdx.x * kFinalCols + threadIdx.x % kFinalCols, run = threadIdx.x / kFinalCols;
   float s = 0.f;
   if (col < c2) {
 #pragma unroll 8
-    for (int b = run; b < a.blocks; b += 16) s += a.partial[static_cast<int64_t>(b) * c2 + col];
+    for (int b = run; b < a.blocks; b += kFinalRuns) s += a.partial[static_cast<int64_t>(b) * c2 + col];
   }
   lds[run][threadIdx.x % kFinalCols] = s;
   __syncthreads();
+  for (int w = kFinalRuns / 2; w > 0; w >>= 1) {
+    if (run < w) lds[run][threadIdx.x % kFinalCols] += lds[run + w][threadIdx.x % kFinalCols];
+    __syncthreads();
+  }
   if (run || col >= c2) return;
-  s = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) s += lds[r][threadIdx.x];
+  s = lds[0][threadIdx.x];
   if (col < a.c) {
     if (a.dgamma) a.dgamma[col] = s;
   } else if (a.dbeta) {
@@ -576,7 +578,7 @@ int launch_layernorm_bwd(const NormArgs &a, int dtype, void *stream) {
   else if (dtype == RT3D_BF16) norm_bwd<__bf16, 8>(a, s);
   else norm_bwd<_Float16, 8>(a, s);
   if (a.partial)
-    layernorm_finalize_kernel<<<(2 * a.c + kFinalCols - 1) / kFinalCols, 256, 0, s>>>(a);
+    layernorm_finalize_kernel<<<(2 * a.c + kFinalCols - 1) / kFinalCols, kFinalCols * kFinalRuns, 0, s>>>(a);
   return hipGetLastError();
 }
 
