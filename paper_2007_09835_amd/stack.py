@@ -2,7 +2,9 @@
 (eight 3x3x3 convs with max-pools), the R(2+1)D-18-shaped stack
 (factorised (2+1)-D convs with residual adds fused into the epilogue) and
 the S3D-shaped stack (Inception blocks whose branches write channel slices
-of one output, separable convs, padded max-pools).
+of one output, separable convs, padded max-pools); and token blocks (layer
+norm, rotary positions, differential attention between 1x1x1 convs) on the
+feature grid that any of them leaves.
 
 Only orchestration lives here: packing at construction, preallocated
 activation buffers, and the sequence of C-ABI launches on one stream (so the
@@ -270,9 +272,108 @@ class S3DStack:
         return self.bufs[self.out_name]
 
 
+class TokenBlock:
+    """One block of token mixing on a feature grid [n][t][h][w][c]:
+
+        u = layer_norm(x),  q, k, v = conv1x1x1(u),  q, k turned by their place,
+        o = differential attention(q, k, v),  y = x + conv1x1x1(layer_norm per head(o)).
+
+    ``heads`` query heads on ``key_heads`` key heads (default: as many) of 2 d =
+    c / heads channels.  ``causal``: a token sees its own frame and earlier ones.
+    Buffers are allocated once, so a pass can be captured in a HIP graph."""
+
+    def __init__(self, c: int, thw, heads: int, key_heads: Optional[int] = None, batch: int = 1,
+                 dtype: str = "bf16", causal: bool = False, depth: int = 0, tag: str = "tokens",
+                 device: str = "cuda"):
+        key_heads = heads if key_heads is None else key_heads
+        if c % (2 * heads) or heads % key_heads:
+            raise ValueError("c must be a multiple of 2 * heads, heads of key_heads")
+        self.c, self.thw, self.heads, self.key_heads, self.batch = c, tuple(thw), heads, key_heads, batch
+        self.dtype = dtype
+        self.d = d = c // (2 * heads)
+        t, h, w = self.thw
+        self.tokens = t * h * w
+        self.frame = h * w if causal else 0
+        # about a quarter of the channels turns with time, the rest with row and column
+        space = 2 * (3 * d // 16)
+        self.sections = (d - 2 * space, space, space)
+        rng = lambda role: synth.rng_for(tag, "block%d" % depth, role)
+        wide = (heads + 2 * key_heads) * 2 * d
+
+        def conv(c_in, c_out, role, residual):
+            wt = synth.to_dtype(rng(role).normal(0.0, c_in ** -0.5, (c_out, c_in, 1, 1, 1)), dtype)
+            bias = rng(role + "_bias").normal(0.0, 0.01, c_out).astype(np.float32)
+            return wt, bias, layers.Conv3d(c_in, c_out, self.thw, (1, 1, 1), (1, 1, 1), (0, 0, 0), wt, bias,
+                                           None, dtype, relu=False, residual=residual, device=device,
+                                           batch=batch)
+
+        self.w_qkv, self.b_qkv, self.qkv = conv(c, wide, "qkv", False)
+        self.w_out, self.b_out, self.proj = conv(c, c, "out", True)
+        vec = lambda role, n, mean, std: torch.from_numpy(
+            rng(role).normal(mean, std, n).astype(np.float32)).to(device)
+        self.gamma, self.beta = vec("gamma", c, 1.0, 0.1), vec("beta", c, 0.0, 0.1)
+        self.head_gamma, self.head_beta = vec("head_gamma", 2 * d, 1.0, 0.1), vec("head_beta", 2 * d, 0.0, 0.1)
+        # the usual start of lambda for a block at this depth
+        self.lam = vec("lambda", heads, 0.8 - 0.6 * float(np.exp(-0.3 * depth)), 0.05)
+        tdt = layers.TORCH_DTYPES[dtype]
+        grid = lambda ch: torch.zeros((batch, *self.thw, ch), dtype=tdt, device=device)
+        self.x, self.normed, self.row = grid(c), grid(c), grid(wide)
+        self.o, self.mixed, self.y = grid(c), grid(c), grid(c)
+        # views of the projected row: queries and keys side by side, then values
+        tokens = self.row.view(batch, self.tokens, wide)
+        nq, nk = heads * 2 * d, key_heads * 2 * d
+        self.turned = tokens[..., :nq + nk].view(batch, self.tokens, (heads + key_heads) * 2, d)
+        self.q = tokens[..., :nq].view(batch, self.tokens, heads, 2, d)
+        self.k = tokens[..., nq:nq + nk].view(batch, self.tokens, key_heads, 2, d)
+        self.v = tokens[..., nq + nk:].view(batch, self.tokens, key_heads, 2 * d)
+
+    def stages(self, x: Optional[torch.Tensor] = None):
+        """(name, fn) of every launch of a pass over ``x`` (default: the input buffer)."""
+        x = self.x if x is None else x
+        heads = lambda b: b.view(self.batch, self.tokens, self.heads, 2 * self.d)
+        return [
+            ("norm", lambda: layers.layer_norm(x, self.gamma, self.beta, out=self.normed)),
+            ("qkv", lambda: self.qkv(self.normed, out=self.row)),
+            ("rope", lambda: layers.rope3d(self.turned, self.thw, self.sections, out=self.turned)),
+            ("attention", lambda: layers.diff_attention(self.q, self.k, self.v, self.lam, self.frame,
+                                                        out=heads(self.o))),
+            ("head_norm", lambda: layers.layer_norm(heads(self.o), self.head_gamma, self.head_beta,
+                                                    out=heads(self.mixed))),
+            ("proj", lambda: self.proj(self.mixed, x, out=self.y)),
+        ]
+
+    def forward(self, x: Optional[torch.Tensor] = None) -> torch.Tensor:
+        for _, launch in self.stages(x):
+            launch()
+        return self.y
+
+
+class TokenStack:
+    """A conv stack with token blocks on its last feature grid."""
+
+    def __init__(self, trunk, blocks: int, heads: int = 8, key_heads: Optional[int] = None,
+                 causal: bool = False, tag: Optional[str] = None):
+        self.trunk, self.net, self.batch, self.dtype = trunk, trunk.net, trunk.batch, trunk.dtype
+        self.x = trunk.x
+        last = list(trunk.bufs.values())[-1] if not hasattr(trunk, "out_name") else trunk.bufs[trunk.out_name]
+        _, t, h, w, c = last.shape
+        self.blocks = [TokenBlock(c, (t, h, w), heads, key_heads, trunk.batch, trunk.dtype, causal, i,
+                                  tag or trunk.net + "-tokens", last.device) for i in range(blocks)]
+
+    def forward(self, x: Optional[torch.Tensor] = None) -> torch.Tensor:
+        y = self.trunk.forward(x)
+        for block in self.blocks:
+            y = block.forward(y)
+        return y
+
+
 def make_stack(net: str, batch: int = 1, dtype: str = "bf16", mode: str = "kgs",
-               rate: float = 3.0, fuse_pool: bool = True, group=(4, 4), streams: int = 2):
-    """The named stack (c3d, r2plus1d or s3d; ``streams`` applies to s3d)."""
+               rate: float = 3.0, fuse_pool: bool = True, group=(4, 4), streams: int = 2,
+               blocks: int = 0):
+    """The named stack (c3d, r2plus1d or s3d; ``streams`` applies to s3d), with
+    ``blocks`` token blocks on its features."""
     if net == "s3d":
-        return S3DStack(batch, dtype, mode, rate, group=group, n_streams=streams)
-    return Stack(net, batch, dtype, mode, rate, fuse_pool=fuse_pool, group=group)
+        trunk = S3DStack(batch, dtype, mode, rate, group=group, n_streams=streams)
+    else:
+        trunk = Stack(net, batch, dtype, mode, rate, fuse_pool=fuse_pool, group=group)
+    return TokenStack(trunk, blocks) if blocks else trunk
