@@ -34,7 +34,8 @@
  *   - Ownership: the caller owns every buffer.  The library never allocates
  *     caller-visible memory, never frees or retains a pointer past a call,
  *     and keeps no state except a thread-local error message, a per-device
- *     cache of runtime queries (compute-unit count, kernel occupancy) and the
+ *     cache of runtime queries and settings (compute-unit count, kernel
+ *     occupancy, the LDS that a kernel may use) and the
  *     split-K scratch array of rt3d_kgs_conv3d_fwd_noalloc (one per device).
  *   - Tuning switch (benchmarks only; leave unset): the environment variable
  *     RT3D_TUNE="key=value,..." overrides planner choices.  Pack-time keys
@@ -384,8 +385,8 @@ rt3d_status rt3d_group_reweight(const rt3d_group_desc *desc, const void *w, cons
  * voxels are tokens.  Token blocks on top of it normalise every vector, project
  * it (1x1x1 convs), rotate queries and keys by the token's place in the grid and
  * attend.  The calls below are those operators and their backward passes.
- * They follow the conventions at the top, except that they need finite values
- * only where they say so, and that pointers of layer norm and of the rotation
+ * They follow the conventions at the top, except that NaN and infinities in a
+ * row go through its own results, and that pointers of layer norm and of the rotation
  * need only the alignment of an element (16-byte aligned pointers and pitches
  * of whole 16 bytes are faster).  Sums, statistics and softmax are float32 with a
  * fixed order: repeated calls give identical results.  Calls may be captured.
@@ -450,9 +451,9 @@ typedef struct {
                                  side) and their channels; d even */
     int32_t dt, dh, dw;       /* channels of the sections, even, at most d together */
     int32_t t0;               /* time of the first frame, for grid positions */
-    float base;               /* > 0 */
     int32_t dtype;            /* rt3d_dtype of x and y */
     uint32_t flags;           /* RT3D_ROPE_HALVES | RT3D_ROPE_INVERSE */
+    double base;              /* > 0 */
     rt3d_rows x, y;           /* rows of vecs * d elements */
 } rt3d_rope_desc;
 

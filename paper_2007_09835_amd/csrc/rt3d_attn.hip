@@ -244,7 +244,8 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
 
   // A row that sees no key, and rows behind the clip's end: zeros, and a
   // logarithm of +inf, which makes every probability of the backward pass zero.
-  const bool any = in && sum[0] > 0.f;
+  // (A sum of NaN is not zero: it goes into the row's results.)
+  const bool any = in && sum[0] != 0.f;
 #pragma unroll
   for (int m = 0; m < kMaps; ++m) {
     const float inv = any ? 1.f / sum[m] : 0.f;
@@ -335,14 +336,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       // a split without keys has weight zero: its results were not written and are not used
-      weight[m][i] = st[i][2 * m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i][2 * m] - top[m]);
+      weight[m][i] = st[i][2 * m + 1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[i][2 * m] - top[m]);
       sum[m] += weight[m][i] * st[i][2 * m + 1];
     }
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1)
 #pragma unroll
     for (int m = 0; m < 2; ++m) sum[m] += __shfl_xor(sum[m], w, 64);
-  const bool any = in && sum[0] > 0.f;
+  const bool any = in && sum[0] != 0.f;
   const float lam = a.lam[head];
   T *o = static_cast<T *>(a.out) + clip * a.o_batch + query * a.o_pitch + static_cast<int64_t>(head) * 2 * a.d;
   T *o2 = static_cast<T *>(a.out2) + ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;

@@ -544,10 +544,11 @@ __global__ __launch_bounds__(1024) void attn_dlam_kernel(AttnArgs a) {
   const int head = blockIdx.x;
   const float *p = a.rowstat + 2 * static_cast<int64_t>(a.n) * a.hq * a.lq;
   float s = 0.f;
-  for (int64_t i = 0; i < static_cast<int64_t>(a.splits) * a.n; ++i) {
-    const float *r = p + (i * a.hq + head) * a.lq;
+  const unsigned len = a.lq, total = static_cast<unsigned>(a.splits) * a.n * len;  // below 2^31 rows
 #pragma unroll 4
-    for (int j = threadIdx.x; j < a.lq; j += 1024) s += r[j];
+  for (unsigned i = threadIdx.x; i < total; i += 1024) {
+    const unsigned part = i / len;
+    s += p[(static_cast<int64_t>(part) * a.hq + head) * len + (i - part * len)];
   }
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);

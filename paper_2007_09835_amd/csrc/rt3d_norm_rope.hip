@@ -556,11 +556,10 @@ void rope_any(const RopeArgs &a, int halves, int pairs, hipStream_t s) {
 
 }  // namespace
 
-int layernorm_bwd_blocks(int64_t rows, int c) {
+int layernorm_bwd_blocks(int64_t rows) {
   // A workgroup's partial sums (2 c floats, written and read) against its rows
   // (3 c elements): at least 16 rows each, and no more than fill the chip.
   const int64_t want = (rows + 15) / 16;
-  (void)c;
   return static_cast<int>(std::min<int64_t>(std::max<int64_t>(want, 1), kNormBlocks));
 }
 

@@ -55,12 +55,12 @@ NormArgs norm_args(const rt3d_norm_desc *d) {
   a.eps = d->eps;
   a.x_pitch = d->x_pitch ? d->x_pitch : d->c;
   a.y_pitch = d->y_pitch ? d->y_pitch : d->c;
-  a.blocks = layernorm_bwd_blocks(d->rows, d->c);
+  a.blocks = layernorm_bwd_blocks(d->rows);
   return a;
 }
 
 uint64_t norm_workspace(const rt3d_norm_desc *d) {
-  return static_cast<uint64_t>(layernorm_bwd_blocks(d->rows, d->c)) * 2 * d->c * sizeof(float);
+  return static_cast<uint64_t>(layernorm_bwd_blocks(d->rows)) * 2 * d->c * sizeof(float);
 }
 
 // ---------------------------------------------------------------------------
@@ -78,7 +78,7 @@ rt3d_status check_rope(const rt3d_rope_desc *d) {
     return fail(RT3D_ERR_INVALID_ARG, "sections pass the vector's %d channels", d->d);
   if (!known_dtype(d->dtype)) return fail(RT3D_ERR_INVALID_ARG, "unknown dtype %d", d->dtype);
   if (d->flags & ~(RT3D_ROPE_HALVES | RT3D_ROPE_INVERSE)) return fail(RT3D_ERR_INVALID_ARG, "unknown flags");
-  if (!(d->base > 0.f) || !std::isfinite(d->base)) return fail(RT3D_ERR_INVALID_ARG, "base must be finite and > 0");
+  if (!(d->base > 0.0) || !std::isfinite(d->base)) return fail(RT3D_ERR_INVALID_ARG, "base must be finite and > 0");
   if (d->t0 < 0 || static_cast<int64_t>(d->t0) + d->t > 0x7fffffffll)
     return fail(RT3D_ERR_INVALID_ARG, "positions t0 .. t0 + t must lie in 0 .. 2^31 - 1");
   const int64_t row = static_cast<int64_t>(d->vecs) * d->d;
@@ -201,8 +201,11 @@ int pick_splits(const rt3d_diffattn_desc *d, int64_t blocks, int64_t steps, doub
     return walk * std::max(1.0, shared * on_cu) + (s > 1 ? 5.0 + 2 * s * part_bytes / 4e6 : 0.0);
   };
   int best = 1;
-  for (int64_t s = 2; s <= most && s <= steps; ++s)
-    if (time(s) < time(best)) best = static_cast<int>(s);
+  double least = time(1);
+  for (int64_t s = 2; s <= most && s <= steps; ++s) {
+    const double t = time(s);
+    if (t < least) least = t, best = static_cast<int>(s);
+  }
   return best;
 }
 
@@ -295,6 +298,8 @@ rt3d_status rt3d_layernorm_fwd(const rt3d_norm_desc *d, const void *x, const flo
       !aligned(rstd, 4))
     return fail(RT3D_ERR_INVALID_ARG, "pointers must be aligned to their element size");
   NormArgs a = norm_args(d);
+  if (x == y && a.x_pitch != a.y_pitch)
+    return fail(RT3D_ERR_INVALID_ARG, "a layer norm in place needs one pitch");
   a.x = x;
   a.y = y;
   a.gamma = gamma;
@@ -362,7 +367,7 @@ rt3d_status rt3d_rope3d(const rt3d_rope_desc *d, const void *x, const int32_t *p
     return fail(RT3D_ERR_INVALID_ARG, "clips of y overlap");
   if (x == y && (a.x_pitch != a.y_pitch || a.x_batch != a.y_batch))
     return fail(RT3D_ERR_INVALID_ARG, "a rotation in place needs one layout");
-  a.base_log2 = std::log2(static_cast<double>(d->base));
+  a.base_log2 = std::log2(d->base);
   a.n = d->n;
   a.h = d->h;
   a.w = d->w;

@@ -65,7 +65,7 @@ struct AttnArgs {
 int launch_layernorm_fwd(const NormArgs &a, int dtype, void *stream);
 int launch_layernorm_bwd(const NormArgs &a, int dtype, void *stream);
 // Workgroups of the backward pass, which is the count of its partial sums.
-int layernorm_bwd_blocks(int64_t rows, int c);
+int layernorm_bwd_blocks(int64_t rows);
 
 int launch_rope(const RopeArgs &a, int dtype, int halves, int pairs, void *stream);
 

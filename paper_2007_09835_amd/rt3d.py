@@ -105,7 +105,7 @@ class Rows(ctypes.Structure):
 class RopeDesc(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in (
         "n", "t", "h", "w", "vecs", "d", "dt", "dh", "dw", "t0")] + [
-        ("base", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("base", ctypes.c_double),
         ("x", Rows), ("y", Rows)]
 
 
@@ -426,7 +426,7 @@ def make_rope_desc(n, grid, vecs, d, sections, dtype="bf16", base=10000.0, t0=0,
     """Fill an rt3d_rope_desc (``x``, ``y``: (pitch, batch) of their rows, tight
     where None)."""
     flags = (RT3D_ROPE_HALVES if halves else 0) | (RT3D_ROPE_INVERSE if inverse else 0)
-    desc = RopeDesc(n, *grid, vecs, d, *sections, t0, base, DTYPE_CODES[dtype], flags)
+    desc = RopeDesc(n, *grid, vecs, d, *sections, t0, DTYPE_CODES[dtype], flags, base)
     _set_rows(desc, {"x": x, "y": y})
     return desc
 

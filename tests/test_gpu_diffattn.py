@@ -217,6 +217,25 @@ def test_gradients_against_differences_of_the_forward_kernel():
             assert abs((hi - lo) / (up - down) - grad.view(-1)[i].item()) <= 3e-3 * max(1.0, grad.abs().max().item())
 
 
+@pytest.mark.parametrize("lq,lk,hq", [(40, 90, 2), (1, 1500, 2)])
+@pytest.mark.parametrize("d", [32, 128])
+def test_nan_stays_in_its_row(lq, lk, hq, d):
+    """A NaN query gives a NaN row (never zeros), the other rows what they gave."""
+    q, k, v, _, lam = _inputs(8, 2, lq, lk, hq, 1, d, "bf16")
+    args = [q[0].cuda(), k[0].cuda(), v[0].cuda(), lam.cuda()]
+    clean = layers.diff_attention(*args)
+    args[0][1, lq // 2, 0, :, 3] = float("nan")
+    got = layers.diff_attention(*args)
+    assert bool(torch.isnan(got[1, lq // 2, 0]).all())
+    got[1, lq // 2, 0] = clean[1, lq // 2, 0]
+    assert torch.equal(got, clean)
+
+
+def test_many_short_clips():
+    """More clips than a workgroup has threads: every sum over the batch takes them all."""
+    _check(51, 1500, 2, 3, 1, 1, 8, "f32", 1)
+
+
 def test_nothing_to_do():
     lam = torch.ones(2, device="cuda")
     e = lambda *s: torch.empty(s, device="cuda", dtype=torch.bfloat16)

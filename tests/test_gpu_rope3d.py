@@ -22,7 +22,7 @@ CASES = [
     (1, (1, 1, 1), 1, 2, (2, 0, 0), 1e4), (2, (2, 3, 5), 3, 32, (8, 12, 12), 1e4),
     (3, (4, 7, 7), 16, 64, (16, 24, 24), 1e4), (1, (3, 2, 2), 5, 80, (20, 20, 20), 500.0),
     (2, (2, 4, 4), 4, 18, (6, 6, 2), 1e4), (1, (2, 5, 3), 7, 128, (32, 48, 48), 1e6),
-    (2, (3, 3, 1), 2, 24, (0, 12, 8), 1e4), (1, (9, 28, 28), 32, 64, (16, 24, 24), 1e4),
+    (2, (3, 3, 1), 2, 24, (0, 12, 8), 1e4), (1, (2, 2, 2), 2, 32, (16, 8, 8), 12345.678901), (1, (9, 28, 28), 32, 64, (16, 24, 24), 1e4),
 ]
 
 

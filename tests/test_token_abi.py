@@ -49,6 +49,9 @@ def test_layer_norm_pointers():
     assert fwd(A, None, None, None, None, None) == INVALID
     assert fwd(A + 1, None, None, A, None, None) == INVALID
     assert fwd(A, A + 2, None, A, None, None) == INVALID
+    d.y_pitch = 16
+    assert fwd(A, None, None, A, None, None) == INVALID  # in place, two pitches
+    d.y_pitch = 0
     assert fwd(A, None, None, A, A + 2, None) == INVALID
     bwd = lambda *a: _status("rt3d_layernorm_bwd", d, *a, None)[0]
     need = rt3d.rt3d_layernorm_bwd_workspace_size(d)
