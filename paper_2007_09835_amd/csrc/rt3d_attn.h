@@ -225,6 +225,26 @@ __device__ __forceinline__ Frag<T> pack(const f32x16 &v, int from) {
   return f;
 }
 
+// acc += a chain of N products whose first operands, read(i), come from LDS up to
+// four products ahead of their use; second(i) is at hand.  (Left to itself the
+// compiler reads, waits and multiplies.  dk/dv has no registers for it: there it
+// spilled and cost 3%.)
+template <typename T, int N, typename R, typename S>
+__device__ __forceinline__ f32x16 chain(R read, S second, f32x16 acc) {
+  constexpr int kRing = N < 4 ? N : 4;
+  Frag<T> f[kRing];
+#pragma unroll
+  for (int i = 0; i < kRing; ++i) f[i] = read(i);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    acc = Mma<T>::run(f[i % kRing], second(i), acc);
+    if (i + kRing < N) f[i % kRing] = read(i + kRing);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  return acc;
+}
+
 // Row of a result register.
 __device__ __forceinline__ int result_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
 

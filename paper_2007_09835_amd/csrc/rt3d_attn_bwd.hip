@@ -134,18 +134,27 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
 #pragma unroll
       for (int j = 0; j < kKeys; j += 32) {
         f32x16 dp = {};
+        if constexpr (sizeof(T) == 2) {
+          dp = chain<T, 2 * D / 16>([&](int i) { return KV::along(vt, j, i * 16); }, [&](int i) { return g[i]; }, dp);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2 * D / 16; ++i) {
-          Frag<T> b;
-          if constexpr (F::kHoldG) b = g[i];
-          else b = grad_frag(i);
-          dp = Mma<T>::run(KV::along(vt, j, i * 16), b, dp);
+          for (int i = 0; i < 2 * D / 16; ++i) {
+            Frag<T> b;
+            if constexpr (F::kHoldG) b = g[i];
+            else b = grad_frag(i);
+            dp = Mma<T>::run(KV::along(vt, j, i * 16), b, dp);
+          }
         }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
           f32x16 s = {};
+          if constexpr (sizeof(T) == 2) {
+            s = chain<T, D / 16>([&](int i) { return KV::along(kt, j, m * D + i * 16); },
+                                 [&](int i) { return q[m][i]; }, s);
+          } else {
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) s = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s);
+            for (int i = 0; i < D / 16; ++i) s = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s);
+          }
           if (masked) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
