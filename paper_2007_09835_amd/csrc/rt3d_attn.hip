@@ -183,11 +183,13 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
 #pragma unroll
         for (int m = 0; m < kMaps; ++m) {
           const float ref = top[m] == -INFINITY ? 0.f : -top[m];
+          float part = 0.f;  // short chains: the sum of a long row keeps its digits
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             s[m][i] = __builtin_amdgcn_exp2f(fmaf(s[m][i], a.scale2, ref));
-            sum[m] += s[m][i];
+            part += s[m][i];
           }
+          sum[m] += part;
         }
         // Rounded to the layer's type for the product with v (half a step of
         // each probability); their sums keep 32 bits.

@@ -122,7 +122,63 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       KV::stage(v + key * a.v_pitch, n, a.d, a.v_pitch, v_off, lds + (buf * 2 + 1) * KV::kBytes);
     };
     const unsigned along = KV::lane_along(), across = KV::lane_across();
+    auto gradients = [&](unsigned vt, int j) {  // dP of 32 keys
+      f32x16 dp = {};
+      if constexpr (sizeof(T) == 2) {
+        dp = chain<T, 2 * D / 16>([&](int i) { return KV::along(vt, j, i * 16); }, [&](int i) { return g[i]; }, dp);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2 * D / 16; ++i) {
+          Frag<T> b;
+          if constexpr (F::kHoldG) b = g[i];
+          else b = grad_frag(i);
+          dp = Mma<T>::run(KV::along(vt, j, i * 16), b, dp);
+        }
+      }
+      return dp;
+    };
+    auto scores = [&](unsigned kt, int key, int j, int m, bool masked) {
+      f32x16 s = {};
+      if constexpr (sizeof(T) == 2) {
+        s = chain<T, D / 16>([&](int i) { return KV::along(kt, j, m * D + i * 16); }, [&](int i) { return q[m][i]; },
+                             s);
+      } else {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) s = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s);
+      }
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key + j + result_row(i, half) >= limit) s[i] = -INFINITY;
+      }
+      return s;
+    };
     stage(begin, 0);
+    // Few keys: the roundings of o and of the probabilities in it do not average
+    // out, and a row sum formed from o is as far off as the differences dP - A are
+    // small (two keys: up to 0.43% of dq and dk in bf16). One tile more of work
+    // sums P dP itself.
+    if (!SPLIT && end <= kKeys) {
+      tile_barrier();
+      const unsigned kt = KV::at(along, lds), vt = KV::at(along, lds + KV::kBytes);
+      mean[0] = mean[1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kKeys; j += 32) {
+        if (j >= wave_end) break;
+        const f32x16 dp = gradients(vt, j);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const f32x16 s = scores(kt, 0, j, m, true);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mean[m] += __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -lse[m])) * dp[i];
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        mean[m] = half_sum(mean[m]);
+        if (in && half == 0) a.rowstat[m * map + stat] = mean[m];
+      }
+    }
     int buf = 0;
     for (int key = begin; key < end; key += kKeys, buf ^= 1) {
       tile_barrier();
@@ -133,33 +189,10 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       const bool masked = key + kKeys > whole;
 #pragma unroll
       for (int j = 0; j < kKeys; j += 32) {
-        f32x16 dp = {};
-        if constexpr (sizeof(T) == 2) {
-          dp = chain<T, 2 * D / 16>([&](int i) { return KV::along(vt, j, i * 16); }, [&](int i) { return g[i]; }, dp);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 2 * D / 16; ++i) {
-            Frag<T> b;
-            if constexpr (F::kHoldG) b = g[i];
-            else b = grad_frag(i);
-            dp = Mma<T>::run(KV::along(vt, j, i * 16), b, dp);
-          }
-        }
+        const f32x16 dp = gradients(vt, j);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-          f32x16 s = {};
-          if constexpr (sizeof(T) == 2) {
-            s = chain<T, D / 16>([&](int i) { return KV::along(kt, j, m * D + i * 16); },
-                                 [&](int i) { return q[m][i]; }, s);
-          } else {
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) s = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s);
-          }
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (key + j + result_row(i, half) >= limit) s[i] = -INFINITY;
-          }
+          f32x16 s = scores(kt, key, j, m, masked);
           float part = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
