@@ -267,8 +267,8 @@ __device__ __forceinline__ int clip_length(const int32_t *len, int clip, int mos
 // Workgroups of one clip and key head read the same keys (or queries): they are
 // dealt to one XCD (ids go round the eight), so that its L2 serves them; or, where
 // that would leave XCDs with unlike work, to all.
-__device__ __forceinline__ int64_t logical_block(const AttnArgs &a) {
-  const int64_t per = (a.blocks + 7) / 8, id = blockIdx.x;
+__device__ __forceinline__ unsigned logical_block(const AttnArgs &a) {
+  const unsigned per = static_cast<unsigned>(a.blocks + 7) / 8, id = blockIdx.x;  // blocks < 2^31
   return a.spread ? id : (id % 8) * per + id / 8;
 }
 inline unsigned grid_of(int64_t blocks) { return static_cast<unsigned>((blocks + 7) / 8 * 8); }

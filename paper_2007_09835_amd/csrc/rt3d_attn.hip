@@ -51,7 +51,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char *lds = (lds_char *)smem;
 
-  int64_t id = logical_block(a);
+  unsigned id = logical_block(a);
   if (id >= a.blocks) return;
   const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
   if (SPLIT) id /= a.splits;

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char *lds = (lds_char *)smem;
 
-  int64_t id = logical_block(a);
+  unsigned id = logical_block(a);
   if (id >= a.blocks) return;
   const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
   if (SPLIT) id /= a.splits;
@@ -259,6 +259,24 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   }
 }
 
+// dlambda of a head, by a workgroup of 256: its rows' sums over the clips and
+// splits, in a fixed order.
+__device__ __forceinline__ void sum_dlam(const AttnArgs &a, int head, float *lds) {
+  const float *p = a.rowstat + 2 * static_cast<int64_t>(a.n) * a.hq * a.lq;
+  const unsigned len = a.lq, total = static_cast<unsigned>(a.stat_splits) * a.n * len;  // below 2^31 rows
+  float s = 0.f;
+#pragma unroll 8
+  for (unsigned i = threadIdx.x; i < total; i += 256) {
+    const unsigned part = i / len;
+    s += p[(static_cast<int64_t>(part) * a.hq + head) * len + (i - part * len)];
+  }
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) a.dlam[head] = 0.f - ((lds[0] + lds[1]) + (lds[2] + lds[3]));
+}
+
 // A lane holds a key: S = Q K^T and dP = dO V^T with the keys and values in
 // registers leave P and dS where dV^T += dO^T P and dK^T += Q^T dS take them.  The
 // heads of a key head's group follow one another and add to the same results.
@@ -292,7 +310,12 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char *lds = (lds_char *)smem;
 
-  int64_t id = logical_block(a);
+  // the last workgroups add up dlambda, which needs no launch of its own then
+  if (blockIdx.x >= gridDim.x - a.dlam_blocks) {
+    sum_dlam(a, static_cast<int>(blockIdx.x - (gridDim.x - a.dlam_blocks)), reinterpret_cast<float *>(smem));
+    return;
+  }
+  unsigned id = logical_block(a);
   if (id >= a.blocks) return;
   const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
   if (SPLIT) id /= a.splits;
@@ -580,27 +603,9 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(AttnArgs a) {
   *reinterpret_cast<Four *>(out + static_cast<int64_t>(head) * 2 * a.d + col) = x;
 }
 
-// dlambda of a head: its rows' sums over the clips and splits, in a fixed order.
-__global__ __launch_bounds__(1024) void attn_dlam_kernel(AttnArgs a) {
-  __shared__ float lds[16];
-  const int head = blockIdx.x;
-  const float *p = a.rowstat + 2 * static_cast<int64_t>(a.n) * a.hq * a.lq;
-  float s = 0.f;
-  const unsigned len = a.lq, total = static_cast<unsigned>(a.splits) * a.n * len;  // below 2^31 rows
-#pragma unroll 4
-  for (unsigned i = threadIdx.x; i < total; i += 1024) {
-    const unsigned part = i / len;
-    s += p[(static_cast<int64_t>(part) * a.hq + head) * len + (i - part * len)];
-  }
-#pragma unroll
-  for (int w = 32; w > 0; w >>= 1) s += __shfl_xor(s, w, 64);
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x) return;
-  s = 0.f;
-#pragma unroll
-  for (int w = 0; w < 16; ++w) s += lds[w];
-  a.dlam[head] = 0.f - s;
+__global__ __launch_bounds__(256) void attn_dlam_kernel(AttnArgs a) {
+  __shared__ float lds[4];
+  sum_dlam(a, blockIdx.x, lds);
 }
 
 template <typename T, int D, bool SPLIT>
@@ -629,7 +634,8 @@ int launch_keys(const AttnArgs &a, hipStream_t s) {
   using F = Dkv<T, D, kWaves>;
   const int e = allow_lds<attn_dkv_kernel<T, D, kWaves, SPLIT, DK, DV>>(F::kLds);
   if (e != hipSuccess) return e;
-  attn_dkv_kernel<T, D, kWaves, SPLIT, DK, DV><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);
+  static_assert(F::kThreads == 256, "sum_dlam's workgroup");
+  attn_dkv_kernel<T, D, kWaves, SPLIT, DK, DV><<<grid_of(a.blocks) + a.dlam_blocks, F::kThreads, F::kLds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -642,7 +648,10 @@ int launch_dkv(AttnArgs a, const BwdPlan &p, hipStream_t s) {
   if (a.blocks == 0) return hipSuccess;
   int e = hipSuccess;
   if constexpr (Dkv<T, D, kBwdRows / 32>::kApart) {
-    if (a.dk) e = launch_keys<T, D, SPLIT, true, false>(a, s);
+    if (a.dk) {
+      e = launch_keys<T, D, SPLIT, true, false>(a, s);
+      a.dlam_blocks = 0;
+    }
     if (e == hipSuccess && a.dv) e = launch_keys<T, D, SPLIT, false, true>(a, s);
   } else {
     e = launch_keys<T, D, SPLIT, true, true>(a, s);
@@ -658,12 +667,14 @@ int launch_dkv(AttnArgs a, const BwdPlan &p, hipStream_t s) {
 template <typename T, int D>
 int bwd(const AttnArgs &a, const BwdPlan &p, hipStream_t s) {
   int e = p.dq_splits > 1 ? launch_dq<T, D, true>(a, p, s) : launch_dq<T, D, false>(a, p, s);
-  if (e == hipSuccess && (a.dk || a.dv))
-    e = p.dkv_splits > 1 ? launch_dkv<T, D, true>(a, p, s) : launch_dkv<T, D, false>(a, p, s);
-  if (e != hipSuccess || !a.dlam) return e;
-  AttnArgs l = a;
-  l.splits = p.dq_splits;
-  attn_dlam_kernel<<<a.hq, 1024, 0, s>>>(l);
+  if (e != hipSuccess) return e;
+  AttnArgs b = a;
+  b.stat_splits = p.dq_splits;
+  if ((a.dk || a.dv) && a.n > 0 && a.lk > 0) {
+    b.dlam_blocks = a.dlam ? a.hq : 0;
+    return p.dkv_splits > 1 ? launch_dkv<T, D, true>(b, p, s) : launch_dkv<T, D, false>(b, p, s);
+  }
+  if (a.dlam) attn_dlam_kernel<<<a.hq, 256, 0, s>>>(b);
   return hipGetLastError();
 }
 

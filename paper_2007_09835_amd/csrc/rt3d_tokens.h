@@ -57,6 +57,8 @@ struct AttnArgs {
   int32_t n, lq, lk, hq, hk, d, group, frame;
   int32_t tiles;              // row (or key) tiles of a (clip, key head)
   int32_t splits, span;       // splits of the other axis and its extent in a split
+  int32_t stat_splits;        // splits of the dq kernel, whose sums of P_2 dP are added up
+  int32_t dlam_blocks;        // workgroups of the dk/dv launch that do so (hq, or 0)
   int32_t spread;             // workgroups of a (clip, key head) go to all XCDs
   float scale, scale2;        // scale2 = scale * log2(e)
 };
