@@ -525,7 +525,7 @@ void norm_bwd(const NormArgs &a, hipStream_t s) {
     layernorm_bwd_kernel<T, V, N, L><<<a.blocks, kNormThreads, 0, s>>>(a);
   });
   if (!done) {
-    if (a.dx)
+    if (a.dx && a.rows > 0)
       layernorm_dx_long_kernel<T, V>
           <<<static_cast<unsigned>(std::min<int64_t>(a.rows, 2 * kNormBlocks)), kNormThreads, 0, s>>>(a);
     if (a.partial)

@@ -88,6 +88,16 @@ def test_no_rows_give_zero_weight_gradients(rows):
     assert dx.shape == x.shape and not dg.any() and not db.any()
 
 
+def test_no_rows_of_any_length():
+    """Also rows too long for registers, which other kernels take."""
+    for c in (32, 2050, 9000, 20001):
+        x = torch.empty(0, c, device="cuda")
+        y, saved = layers.layer_norm(x, save=True)
+        dx, dg, db = layers.layer_norm_backward(y, x, None, saved)
+        torch.cuda.synchronize()
+        assert dx.shape == x.shape and dg.shape == db.shape == (c,) and not dg.any() and not db.any()
+
+
 def test_a_constant_row_and_repeated_calls():
     x = torch.full((3, 512), 3.0, device="cuda", dtype=torch.float16)
     y, saved = layers.layer_norm(x, save=True)
