@@ -494,8 +494,9 @@ rt3d_status rt3d_diffattn_fwd_workspace_size(const rt3d_diffattn_desc *desc, uin
 /* lambda: float32 [hq].  q_len, k_len: int32 [n] device arrays, or NULL (lq, lk);
  * values outside 0 .. lq (lk) count as the nearest bound.  Queries behind q_len
  * and keys and values behind k_len are never read and may hold anything; o is
- * zero in rows behind q_len.  Values of keys that only the frame mask hides must
- * be finite.  o2 and lse are what the backward pass needs, or NULL: o2 the second
+ * zero in rows behind q_len.  Keys that only the frame mask hides are read with
+ * the others of their tile: a value there must be finite (as zero times it is added),
+ * and for the backward pass so must keys, queries and output gradients.  o2 and lse are what the backward pass needs, or NULL: o2 the second
  * map's output P_2 v, tight [n][lq][hq][2 d] in desc->dtype, lse float32
  * [2][n][hq][lq], the base-2 logarithm of each map's softmax denominator.
  * Pointers must be 16-byte aligned (lambda, lse and lengths 4), pitches and batch

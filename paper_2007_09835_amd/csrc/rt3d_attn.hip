@@ -373,7 +373,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
           for (int j = 0; j < 8; ++j) {
             const int s = s0 + j * SHARE;
             const float w0 = __shfl(weight[0][i], s, 64), w1 = __shfl(weight[1][i], s, 64), by = m ? w1 : w0;
-            if (s < n && w0 != 0.f) {
+            if (s < n && by != 0.f) {  // (one map's weight may vanish alone)
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] += by * x[j][e];
             }

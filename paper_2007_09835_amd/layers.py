@@ -278,7 +278,8 @@ def diff_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch
     """Differential attention: q [n, lq, hq, 2, d], k [n, lk, hk, 2, d], v [n, lk,
     hk, 2 d], lam float32 [hq] -> [n, lq, hq, 2 d].  ``frame`` tokens make a frame of
     the causal mask (0: none); ``q_len``, ``k_len`` (int32 [n]): the clips' lengths in
-    a padded batch or a cache.  With ``save`` also what
+    a padded batch or a cache; what lies behind them may be anything, but what only
+    the frames' mask hides must be finite.  With ``save`` also what
     ``diff_attention_backward`` needs."""
     desc = _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=out)
     n, lq, hq, _, d = q.shape

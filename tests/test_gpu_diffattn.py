@@ -147,6 +147,27 @@ def test_scores_that_rise_along_the_keys():
     refs.within(o, ref["o"], ref["o_err"], "o")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_splits_whose_weight_vanishes_in_one_map(dtype):
+    """The second half of the cache takes all of the first map (its scores lie 400
+    above the others: their probabilities are zero in 32 bits) and leaves the second
+    map, whose scores are ordinary, to both halves."""
+    n, lk, d = 1, 2048, 32
+    q, k, v, _, lam = _inputs(61, n, 1, lk, 1, 1, d, dtype)
+    for qq in q:
+        qq[0, 0, 0, 0] = 0.0
+        qq[0, 0, 0, 0, 0] = 16.0
+    for kk in k:
+        kk[0, :lk // 2, 0, 0, 0] = 0.0
+        kk[0, lk // 2:, 0, 0, 0] = 25.0
+    o, saved = layers.diff_attention(q[0].cuda(), k[0].cuda(), v[0].cuda(), lam.cuda(), scale=1.0, save=True)
+    h = 0.0 if dtype == "f32" else refs.HALF[dtype]
+    ref = refs.diff_attention(q[1], k[1], v[1], lam.double(), scale=1.0, h=h, tiny=refs.TINY[dtype])
+    half = refs.U if dtype == "f32" else 0.0
+    refs.within(o, ref["o"], ref["o_err"] + half * ref["o"].abs() + 1e-30, "o")
+    refs.within(saved[1], ref["o2"], ref["o2_err"] + half * ref["o2"].abs() + 1e-30, "o2")
+
+
 def test_repeated_calls_and_other_streams():
     q, k, v, do, lam = _inputs(7, 2, 150, 150, 4, 2, 64, "bf16")
     args = [t[0].cuda() for t in (q, k, v)] + [lam.cuda()]
