@@ -29,7 +29,7 @@ struct Fwd {
   static constexpr int kWidth = 2 * D;
   using KV = Tile<T, D, kKeys, kThreads>;
   static constexpr int kLds = 4 * KV::kBytes;
-  static constexpr int kMinWaves = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kMinWaves = sizeof(T) == 2 || D <= 32 ? 2 : 1;
   // operands read ahead of their products: registers for them are left in 16 bits
   static constexpr bool kAhead = sizeof(T) == 2;
   // The transposing reads wait for every load under way: the next tile's loads
@@ -38,9 +38,11 @@ struct Fwd {
   static_assert(kMaps == 2 || ROWS * 32 * kWidth * 4 <= kLds, "the second maps' results fit");
 };
 
-// log2 units by which a row's scores may pass its reference before everything is
-// scaled down to a new one: P <= 2^8 fits every type, and most tiles need no pass.
-constexpr float kSlack = 8.f;
+// A row's reference is the maximum of its first 32 keys, and no maximum is formed
+// after that: a step whose probabilities against the reference add up to more than
+// this (in a lane, 16 keys) is done again with a new one, everything before it scaled
+// down.  P up to 2^8 fits every type, and steps after the first hardly ever get there.
+constexpr float kMost = 256.f;
 
 template <typename T, int D, int ROWS, bool SPLIT>
 __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMinWaves)) void attn_fwd_kernel(
@@ -108,6 +110,51 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
     };
     // (a second map's vectors begin a whole number of 16 blocks on: beyond d = 64)
     const unsigned k_lane = KV::lane_along() + map0 * D * KV::kEs, v_lane = KV::lane_across();
+    using Scores = f32x16[kMaps];
+    auto scores = [&](Scores &s, unsigned kt, int j) {
+#pragma unroll
+      for (int m = 0; m < kMaps; ++m)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) s[m] = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s[m]);
+    };
+    auto hide = [&](Scores &s, int key) {
+#pragma unroll
+      for (int m = 0; m < kMaps; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key + result_row(i, half) >= limit) s[m][i] = -INFINITY;
+    };
+    auto raise = [&](const Scores &s) {  // the reference, to the maximum so far
+#pragma unroll
+      for (int m = 0; m < kMaps; ++m) {
+        float most = s[m][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, s[m][i]);
+        const float now = fmaxf(top[m], half_max(most) * a.scale2);
+        const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
+        top[m] = now;
+        sum[m] *= by;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[m][t][i] *= by;
+      }
+    };
+    auto probabilities = [&](Scores &s, float (&part)[kMaps]) {
+      bool over = false;
+#pragma unroll
+      for (int m = 0; m < kMaps; ++m) {
+        const float ref = top[m] == -INFINITY ? 0.f : -top[m];
+        part[m] = 0.f;  // short chains: the sum of a long row keeps its digits
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[m][i] = __builtin_amdgcn_exp2f(fmaf(s[m][i], a.scale2, ref));
+          part[m] += s[m][i];
+        }
+        over |= part[m] > kMost;
+      }
+      return over;
+    };
     stage(begin, 0);
     int buf = 0;
     for (int tile_key = begin; tile_key < end; tile_key += kKeys, buf ^= 1) {
@@ -138,10 +185,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
             __builtin_amdgcn_sched_barrier(0);
           }
         } else {
-#pragma unroll
-          for (int m = 0; m < kMaps; ++m)
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) s[m] = Mma<T>::run(KV::along(kt, j, m * D + i * 16), q[m][i], s[m]);
+          scores(s, kt, j);
         }
         Frag<T> v0[kTiles];  // values of the first 16 keys, on their way during the softmax
         if constexpr (F::kAhead) {
@@ -150,47 +194,21 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
           __builtin_amdgcn_sched_barrier(0);
         }
         if (F::kLate && j == 0 && more) stage(tile_key + kKeys, buf ^ 1);
-        if (key + 32 > whole) {
+        if (key + 32 > whole) hide(s, key);
+        const bool start = key == begin;
+        if (start) raise(s);
+        float part[kMaps];
+        bool over = probabilities(s, part);
+        if (__builtin_expect(!start && __any(over), 0)) {
 #pragma unroll
-          for (int m = 0; m < kMaps; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (key + result_row(i, half) >= limit) s[m][i] = -INFINITY;
-        }
-        float most[kMaps];
-        bool up = false;
-#pragma unroll
-        for (int m = 0; m < kMaps; ++m) {
-          most[m] = s[m][0];
-#pragma unroll
-          for (int i = 1; i < 16; ++i) most[m] = fmaxf(most[m], s[m][i]);
-          most[m] = half_max(most[m]) * a.scale2;
-          up |= most[m] > top[m] + kSlack;
-        }
-        if (__any(up)) {
-#pragma unroll
-          for (int m = 0; m < kMaps; ++m) {
-            const float now = fmaxf(top[m], most[m]);
-            const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
-            top[m] = now;
-            sum[m] *= by;
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) acc[m][t][i] *= by;
-          }
+          for (int m = 0; m < kMaps; ++m) s[m] = f32x16{};
+          scores(s, kt, j);
+          if (key + 32 > whole) hide(s, key);
+          raise(s);
+          probabilities(s, part);
         }
 #pragma unroll
-        for (int m = 0; m < kMaps; ++m) {
-          const float ref = top[m] == -INFINITY ? 0.f : -top[m];
-          float part = 0.f;  // short chains: the sum of a long row keeps its digits
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            s[m][i] = __builtin_amdgcn_exp2f(fmaf(s[m][i], a.scale2, ref));
-            part += s[m][i];
-          }
-          sum[m] += part;
-        }
+        for (int m = 0; m < kMaps; ++m) sum[m] += part[m];
         // Rounded to the layer's type for the product with v (half a step of
         // each probability); their sums keep 32 bits.
         Frag<T> p[kMaps][2];
