@@ -264,12 +264,44 @@ __device__ __forceinline__ int clip_length(const int32_t *len, int clip, int mos
   return v < 0 ? 0 : v > most ? most : v;
 }
 
-// Workgroups of one clip and key head read the same keys (or queries): they are
-// dealt to one XCD (ids go round the eight), so that its L2 serves them; or, where
-// that would leave XCDs with unlike work, to all.
-__device__ __forceinline__ unsigned logical_block(const AttnArgs &a) {
-  const unsigned per = static_cast<unsigned>(a.blocks + 7) / 8, id = blockIdx.x;  // blocks < 2^31
-  return a.spread ? id : (id % 8) * per + id / 8;
+// What a workgroup does: tile number `rank` of those of a pair (clip, key head), in
+// the order of their work, and which split of it.
+struct Place {
+  int split, rank, kvh, clip;
+};
+
+// Workgroups of a pair read the same keys (or queries).  Without a causal mask they
+// follow one another on one XCD (ids go round the eight), whose L2 then serves them;
+// or, where clips of unlike lengths would leave XCDs with unlike work, on all.  With
+// one, the tiles with most work of all pairs come first, so that the last ones to
+// start are short: the pairs are dealt to the XCDs in as many sets as divide both.
+// (16 pairs of 1568 tokens SIM)
+// False: the workgroup has no work.
+__device__ __forceinline__ bool place(const AttnArgs &a, Place &p) {
+  unsigned id = blockIdx.x;
+  if (!a.sets && !a.spread) {
+    const unsigned per = static_cast<unsigned>(a.blocks + 7) / 8;  // blocks < 2^31
+    id = (id % 8) * per + id / 8;
+  }
+  if (id >= a.blocks) return false;
+  const unsigned splits = a.splits, tiles = a.tiles;
+  unsigned pair;
+  if (a.sets) {
+    const unsigned sets = a.sets, pairs = static_cast<unsigned>(a.n) * a.hk / sets, set = id % sets;
+    id /= sets;
+    p.split = static_cast<int>(id % splits);
+    id /= splits;
+    p.rank = static_cast<int>(id / pairs);
+    pair = set * pairs + id % pairs;
+  } else {
+    p.split = static_cast<int>(id % splits);
+    id /= splits;
+    p.rank = static_cast<int>(id % tiles);
+    pair = id / tiles;
+  }
+  p.clip = static_cast<int>(pair / a.hk);
+  p.kvh = static_cast<int>(pair - static_cast<unsigned>(p.clip) * a.hk);
+  return true;
 }
 inline unsigned grid_of(int64_t blocks) { return static_cast<unsigned>((blocks + 7) / 8 * 8); }
 

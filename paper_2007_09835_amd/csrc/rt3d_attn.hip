@@ -58,13 +58,10 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char *lds = (lds_char *)smem;
 
-  unsigned id = logical_block(a);
-  if (id >= a.blocks) return;
-  const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
-  if (SPLIT) id /= a.splits;
-  const int tile = a.tiles - 1 - static_cast<int>(id % a.tiles);  // rows with most keys first
-  id /= a.tiles;
-  const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
+  Place here;
+  if (!place(a, here)) return;
+  const int split = SPLIT ? here.split : 0, kvh = here.kvh, clip = here.clip;
+  const int tile = a.tiles - 1 - here.rank;  // rows with most keys first
 
   const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);
   const int rows = a.lq * a.group, used = q_len * a.group;
@@ -320,10 +317,10 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
       if (a.out2 && map0 == kMaps % 2) *reinterpret_cast<Four *>(o2 + col) = y;
     }
   if (a.lse && half == 0) {
-    const int64_t at = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
+    const int64_t stat = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
 #pragma unroll
     for (int m = 0; m < kMaps; ++m)
-      a.lse[(map0 + m) * static_cast<int64_t>(a.n) * a.hq * a.lq + at] = any ? top[m] + log2f(sum[m]) : INFINITY;
+      a.lse[(map0 + m) * static_cast<int64_t>(a.n) * a.hq * a.lq + stat] = any ? top[m] + log2f(sum[m]) : INFINITY;
   }
 }
 

@@ -38,13 +38,10 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   lds_char *lds = (lds_char *)smem;
 
-  unsigned id = logical_block(a);
-  if (id >= a.blocks) return;
-  const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
-  if (SPLIT) id /= a.splits;
-  const int tile = a.tiles - 1 - static_cast<int>(id % a.tiles);
-  id /= a.tiles;
-  const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
+  Place here;
+  if (!place(a, here)) return;
+  const int split = SPLIT ? here.split : 0, kvh = here.kvh, clip = here.clip;
+  const int tile = a.tiles - 1 - here.rank;  // rows with most keys first
   const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);
   const int rows = a.lq * a.group, used = q_len * a.group;
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(static_cast<int>(threadIdx.x) >> 6);
@@ -315,13 +312,10 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
     sum_dlam(a, static_cast<int>(blockIdx.x - (gridDim.x - a.dlam_blocks)), reinterpret_cast<float *>(smem));
     return;
   }
-  unsigned id = logical_block(a);
-  if (id >= a.blocks) return;
-  const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
-  if (SPLIT) id /= a.splits;
-  const int tile = static_cast<int>(id % a.tiles);  // keys that most queries see first
-  id /= a.tiles;
-  const int kvh = static_cast<int>(id % a.hk), clip = static_cast<int>(id / a.hk);
+  Place here;
+  if (!place(a, here)) return;
+  const int split = SPLIT ? here.split : 0, kvh = here.kvh, clip = here.clip;
+  const int tile = here.rank;  // keys that most queries see first
   const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(static_cast<int>(threadIdx.x) >> 6);
   const int key_block = tile * WAVES * 32, key_wave = key_block + wave * 32, key = key_wave + (lane & 31);

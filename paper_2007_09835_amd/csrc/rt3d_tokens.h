@@ -60,6 +60,7 @@ struct AttnArgs {
   int32_t stat_splits;        // splits of the dq kernel, whose sums of P_2 dP are added up
   int32_t dlam_blocks;        // workgroups of the dk/dv launch that do so (hq, or 0)
   int32_t spread;             // workgroups of a (clip, key head) go to all XCDs
+  int32_t sets;               // causal: (clip, key head) pairs are this many sets, dealt to the XCDs; else 0
   float scale, scale2;        // scale2 = scale * log2(e)
 };
 
@@ -78,7 +79,7 @@ int launch_attn_fwd(const AttnArgs &a, int dtype, int row_groups, void *stream);
 // Splits of the backward kernels' walks (keys for dq, query tiles for dk and dv),
 // and where their partial results lie in the workspace (floats).
 struct BwdPlan {
-  int dq_splits, dq_span, dkv_splits, dkv_span;
+  int dq_splits, dq_span, dkv_splits;
   uint64_t dq_part, dkv_part, floats;
 };
 constexpr int kBwdRows = 128;  // rows (keys) of a backward workgroup
