@@ -59,7 +59,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
   lds_char *lds = (lds_char *)smem;
 
   Place here;
-  if (!place(a, here)) return;
+  if (!place(a, a.k_len, a.lk, here)) return;
   const int split = SPLIT ? here.split : 0, kvh = here.kvh, clip = here.clip;
   const int tile = a.tiles - 1 - here.rank;  // rows with most keys first
 

@@ -39,7 +39,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
   lds_char *lds = (lds_char *)smem;
 
   Place here;
-  if (!place(a, here)) return;
+  if (!place(a, a.k_len, a.lk, here)) return;
   const int split = SPLIT ? here.split : 0, kvh = here.kvh, clip = here.clip;
   const int tile = a.tiles - 1 - here.rank;  // rows with most keys first
   const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
     return;
   }
   Place here;
-  if (!place(a, here)) return;
+  if (!place(a, a.q_len, a.lq, here)) return;
   const int split = SPLIT ? here.split : 0, kvh = here.kvh, clip = here.clip;
   const int tile = here.rank;  // keys that most queries see first
   const int q_len = clip_length(a.q_len, clip, a.lq), k_len = clip_length(a.k_len, clip, a.lk);

@@ -168,6 +168,28 @@ def test_splits_whose_weight_vanishes_in_one_map(dtype):
     refs.within(saved[1], ref["o2"], ref["o2_err"] + half * ref["o2"].abs() + 1e-30, "o2")
 
 
+@pytest.mark.parametrize("n,frame", [(5, 0), (64, 0), (65, 0), (5, 3), (24, 1)])
+def test_clips_in_any_order(n, frame):
+    """A batch in another order gives the same bits in that order, whatever order its
+    clips are worked on: equal and zero lengths, lengths out of range, more clips than a
+    wave has lanes."""
+    lq, lk, hq, hk, d = 140, 150, 4, 2, 16
+    q, k, v, do, lam = (t if torch.is_tensor(t) else t[0] for t in _inputs(71, n, lq, lk, hq, hk, d, "bf16"))
+    gen = torch.Generator().manual_seed(n)
+    q_len, k_len = (torch.randint(-3, m + 6, (n,), generator=gen).int() for m in (lq, lk))
+    q_len[1], k_len[1] = q_len[0], k_len[0]
+
+    def run(order):
+        args = [t[order].cuda() for t in (q, k, v)] + [lam.cuda()]
+        more = dict(frame=frame, q_len=q_len[order].cuda(), k_len=k_len[order].cuda())
+        o, saved = layers.diff_attention(*args, save=True, **more)
+        return (o, *layers.diff_attention_backward(do[order].cuda(), *args, saved, **more)[:3])
+
+    order = torch.randperm(n, generator=gen)
+    for a, b in zip(run(torch.arange(n)), run(order)):
+        assert torch.equal(a[order.cuda()], b)
+
+
 def test_repeated_calls_and_other_streams():
     q, k, v, do, lam = _inputs(7, 2, 150, 150, 4, 2, 64, "bf16")
     args = [t[0].cuda() for t in (q, k, v)] + [lam.cuda()]
