@@ -170,11 +170,11 @@ def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None,
     _need(out, "out", x, x.shape, x.dtype)
 
     def call():
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        y = x.new_empty(x.shape) if out is None else out
         rows = x.numel() // c if c else 0
         mean = rstd = None
         if save:
-            mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind()
+            mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind()
         d = rt3d.make_norm_desc(rows, c, dtype, eps, _row_pitch(x, "x"), _row_pitch(y, "out"))
         rt3d.rt3d_layernorm_fwd(d, x, gamma, beta, y, mean, rstd)
         return (y, (mean, rstd)) if save else y
@@ -197,10 +197,9 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch
 
     def call():
         d = rt3d.make_norm_desc(rows, c, dtype, 1.0, _row_pitch(x, "x"), _row_pitch(dy, "dy"))
-        dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
-        dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=x.device).unbind()
-        ws = torch.empty(rt3d.rt3d_layernorm_bwd_workspace_size(d) // 4, dtype=torch.float32,
-                         device=x.device)
+        dx = x.new_empty_strided(x.shape, x.stride())
+        dgamma, dbeta = x.new_empty((2, c), dtype=torch.float32).unbind()
+        ws = x.new_empty(rt3d.rt3d_layernorm_bwd_workspace_size(d) // 4, dtype=torch.float32)
         rt3d.rt3d_layernorm_bwd(d, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws)
         return dx, dgamma, dbeta
 
@@ -212,15 +211,17 @@ def _rows_of(x: torch.Tensor, width: int, name: str):
     dense elements; None where it is tight."""
     if x.is_contiguous():
         return None
+    sizes, steps = x.shape, x.stride()
     inner = 1
-    for size, step in zip(reversed(x.shape[2:]), reversed(x.stride()[2:])):
-        if size != 1 and step != inner:
+    for i in range(len(sizes) - 1, 1, -1):
+        size = sizes[i]
+        if size != 1 and steps[i] != inner:
             raise ValueError("%s: a token's vectors must be dense" % name)
         inner *= size
-    pitch = x.stride(1) if x.shape[1] > 1 else width
-    if pitch < width or (x.shape[0] > 1 and x.stride(0) <= 0 and x.numel()):
+    pitch = steps[1] if sizes[1] > 1 else width
+    if pitch < width or (sizes[0] > 1 and steps[0] <= 0 and x.numel()):
         raise ValueError("%s: its tokens or clips share memory" % name)
-    return pitch, x.stride(0) if x.shape[0] > 1 else 0
+    return pitch, steps[0] if sizes[0] > 1 else 0
 
 
 def rope3d(x: torch.Tensor, grid: Sequence[int], sections: Sequence[int], base: float = 10000.0,
@@ -240,7 +241,7 @@ def rope3d(x: torch.Tensor, grid: Sequence[int], sections: Sequence[int], base: 
     _need(pos, "pos", x, (n, tokens, 3), torch.int32)
 
     def call():
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        y = x.new_empty(x.shape) if out is None else out
         desc = rt3d.make_rope_desc(n, grid, vecs, d, sections, dtype, base, t0, halves, inverse,
                                    _rows_of(x, vecs * d, "x"), _rows_of(y, vecs * d, "out"))
         rt3d.rt3d_rope3d(desc, x, pos, y)
@@ -249,8 +250,8 @@ def rope3d(x: torch.Tensor, grid: Sequence[int], sections: Sequence[int], base: 
     return _launch(x, stream, call)
 
 
-def _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, **more):
-    """Checks the inputs of differential attention and fills their descriptor."""
+def _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=None, d_o=None):
+    """Checks the tensors of differential attention and fills its descriptor."""
     if q.dim() != 5 or q.shape[3] != 2:
         raise ValueError("q must be [n, lq, hq, 2, d], not %s" % list(q.shape))
     n, lq, hq, _, d = q.shape
@@ -262,13 +263,16 @@ def _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, **more):
     _need(lam, "lam", q, (hq,), torch.float32)
     _need(q_len, "q_len", q, (n,), torch.int32)
     _need(k_len, "k_len", q, (n,), torch.int32)
-    rows = {"q": _rows_of(q, hq * 2 * d, "q"), "k": _rows_of(k, hk * 2 * d, "k"),
-            "v": _rows_of(v, hk * 2 * d, "v")}
-    for name, t in more.items():
-        if t is not None:
-            rows[name] = _rows_of(t, t.shape[2] * 2 * d, name)
-    return rt3d.make_diffattn_desc(n, lq, lk, hq, hk, d, _dtype_of(q, "q"), frame,
-                                   0.0 if scale is None else scale, **rows)
+    _need(o, "out", q, (n, lq, hq, 2 * d), q.dtype)
+    _need(d_o, "do", q, (n, lq, hq, 2 * d), q.dtype)
+    if scale is not None and not scale > 0:
+        raise ValueError("scale must be > 0 (None: 1 / sqrt(d)), got %s" % scale)
+    row_q, row_k = hq * 2 * d, hk * 2 * d
+    return rt3d.make_diffattn_desc(n, lq, lk, hq, hk, d, _dtype_of(q, "q"), frame, scale or 0.0,
+                                   q=_rows_of(q, row_q, "q"), k=_rows_of(k, row_k, "k"),
+                                   v=_rows_of(v, row_k, "v"),
+                                   o=None if o is None else _rows_of(o, row_q, "out"),
+                                   d_o=None if d_o is None else _rows_of(d_o, row_q, "do"))
 
 
 def diff_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor,
@@ -284,17 +288,16 @@ def diff_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch
     desc = _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=out)
     n, lq, hq, _, d = q.shape
     shape = (n, lq, hq, 2 * d)
-    _need(out, "out", q, shape, q.dtype)
 
     def call():
-        o = torch.empty(shape, dtype=q.dtype, device=q.device) if out is None else out
+        o = q.new_empty(shape) if out is None else out
         o2 = lse = ws = None
         if save:
-            o2 = torch.empty(shape, dtype=q.dtype, device=q.device)
-            lse = torch.empty((2, n, hq, lq), dtype=torch.float32, device=q.device)
+            o2 = q.new_empty(shape)
+            lse = q.new_empty((2, n, hq, lq), dtype=torch.float32)
         nbytes = rt3d.rt3d_diffattn_fwd_workspace_size(desc)
         if nbytes:
-            ws = torch.empty(nbytes // 4, dtype=torch.float32, device=q.device)
+            ws = q.new_empty(nbytes // 4, dtype=torch.float32)
         rt3d.rt3d_diffattn_fwd(desc, q, k, v, lam, q_len, k_len, o, o2, lse, ws)
         return (o, (o, o2, lse)) if save else o
 
@@ -309,18 +312,16 @@ def diff_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, 
     """(dq, dk, dv, dlam) of ``diff_attention(..., save=True)`` with the same
     arguments."""
     o, o2, lse = saved
-    n, lq, hq, _, d = q.shape
-    _need(do, "do", q, (n, lq, hq, 2 * d), q.dtype)
-    _need(o, "o", q, do.shape, q.dtype)
+    desc = _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=o, d_o=do)
+    n, lq, hq = q.shape[:3]
     _need(o2, "o2", q, do.shape, q.dtype)
     _need(lse, "lse", q, (2, n, hq, lq), torch.float32)
-    desc = _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=o, d_o=do)
 
     def call():
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        dlam = torch.empty(hq, dtype=torch.float32, device=q.device)
+        dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+        dlam = lam.new_empty(hq)
         nbytes = rt3d.rt3d_diffattn_bwd_workspace_size(desc)
-        ws = torch.empty(nbytes // 4, dtype=torch.float32, device=q.device) if nbytes else None
+        ws = q.new_empty(nbytes // 4, dtype=torch.float32) if nbytes else None
         rt3d.rt3d_diffattn_bwd(desc, q, k, v, lam, q_len, k_len, o, o2, lse, do, dq, dk, dv, dlam, ws)
         return dq, dk, dv, dlam
 

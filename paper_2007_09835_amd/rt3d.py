@@ -421,20 +421,16 @@ def rt3d_layernorm_bwd(desc: NormDesc, x, dy, gamma, mean, rstd, dx=None, dgamma
         _dev_ptr(dgamma, "dgamma"), _dev_ptr(dbeta, "dbeta"), *_ws(workspace), _stream_ptr(stream)))
 
 
+_TIGHT = (0, 0)
+
+
 def make_rope_desc(n, grid, vecs, d, sections, dtype="bf16", base=10000.0, t0=0, halves=False,
                    inverse=False, x=None, y=None) -> RopeDesc:
     """Fill an rt3d_rope_desc (``x``, ``y``: (pitch, batch) of their rows, tight
     where None)."""
     flags = (RT3D_ROPE_HALVES if halves else 0) | (RT3D_ROPE_INVERSE if inverse else 0)
-    desc = RopeDesc(n, *grid, vecs, d, *sections, t0, DTYPE_CODES[dtype], flags, base)
-    _set_rows(desc, {"x": x, "y": y})
-    return desc
-
-
-def _set_rows(desc, rows) -> None:
-    for name, layout in rows.items():
-        if layout is not None:
-            setattr(desc, name, Rows(*layout))
+    return RopeDesc(n, *grid, vecs, d, *sections, t0, DTYPE_CODES[dtype], flags, base,
+                    x or _TIGHT, y or _TIGHT)
 
 
 def rt3d_rope3d(desc: RopeDesc, x, pos, y, stream=None) -> None:
@@ -442,12 +438,13 @@ def rt3d_rope3d(desc: RopeDesc, x, pos, y, stream=None) -> None:
                               _view_ptr(y, "y"), _stream_ptr(stream)))
 
 
-def make_diffattn_desc(n, lq, lk, hq, hk, d, dtype="bf16", frame=0, scale=0.0, **rows) -> DiffAttnDesc:
-    """Fill an rt3d_diffattn_desc; ``rows``: (pitch, batch) by tensor (q, o, k,
-    v, d_o, dq, dk, dv), tight where absent or None."""
-    desc = DiffAttnDesc(n, lq, lk, hq, hk, d, DTYPE_CODES[dtype], frame, scale)
-    _set_rows(desc, rows)
-    return desc
+def make_diffattn_desc(n, lq, lk, hq, hk, d, dtype="bf16", frame=0, scale=0.0, q=None, o=None,
+                       k=None, v=None, d_o=None, dq=None, dk=None, dv=None) -> DiffAttnDesc:
+    """Fill an rt3d_diffattn_desc; ``q`` to ``dv``: (pitch, batch) of a tensor's
+    rows, tight where None."""
+    return DiffAttnDesc(n, lq, lk, hq, hk, d, DTYPE_CODES[dtype], frame, scale, q or _TIGHT,
+                        o or _TIGHT, k or _TIGHT, v or _TIGHT, d_o or _TIGHT, dq or _TIGHT,
+                        dk or _TIGHT, dv or _TIGHT)
 
 
 def rt3d_diffattn_fwd_workspace_size(desc: DiffAttnDesc) -> int:

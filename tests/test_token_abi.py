@@ -210,3 +210,24 @@ def test_the_layers_refuse_what_a_pointer_would_not_show():
         with pytest.raises(ValueError):
             layers._row_pitch(rows, "x")
     assert layers._row_pitch(t(3, 4, 10)[..., :8], "x") == 10
+
+
+def test_a_scale_of_zero_is_no_default():
+    """None asks for 1 / sqrt(d); a number has to be a scale.  An ``out`` of any
+    other shape is refused before its strides are looked at."""
+    t = torch.empty
+    q, k, v, lam = t(2, 3, 4, 2, 16), t(2, 5, 2, 2, 16), t(2, 5, 2, 32), t(4)
+    for scale in (0.0, -1.0, float("nan")):
+        with pytest.raises(ValueError, match="scale"):
+            layers.diff_attention(q, k, v, lam, scale=scale)
+    for out in (t(2, 3), t(2, 3, 4, 16), t(2, 3, 4, 32, dtype=torch.float16)):
+        with pytest.raises(ValueError, match="out"):
+            layers.diff_attention(q, k, v, lam, out=out)
+
+
+def test_descriptors_hold_the_rows_they_are_given():
+    d = rt3d.make_diffattn_desc(1, 2, 3, 4, 2, 16, q=(130, 0), dv=(72, 640))
+    assert (d.q.pitch, d.q.batch, d.dv.pitch, d.dv.batch) == (130, 0, 72, 640)
+    assert all(r.pitch == r.batch == 0 for r in (d.o, d.k, d.v, d.d_o, d.dq, d.dk))
+    r = rt3d.make_rope_desc(1, (1, 2, 3), 2, 8, (2, 2, 2), y=(24, 144))
+    assert (r.x.pitch, r.x.batch, r.y.pitch, r.y.batch) == (0, 0, 24, 144)
