@@ -25,6 +25,10 @@ struct Dq {
   // 32-bit output gradients of 256 columns beside the queries pass the register
   // file: they are read again for every step, from L1.
   static constexpr bool kHoldG = sizeof(T) == 2 || D <= 64;
+  // As in the forward pass, one of a SIMD's two waves should multiply while the
+  // other forms probabilities, which go first, then scores, then the products of
+  // the gradient.  (2 clips of 6272 tokens, 8 heads, d 64, causal: 369 us without, 340.)
+  static constexpr bool kTurns = sizeof(T) == 2;
 };
 
 // Rows of queries as in the forward pass (a lane holds a row): S^T = K Q^T and
@@ -186,10 +190,13 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       const bool masked = key + kKeys > whole;
 #pragma unroll
       for (int j = 0; j < kKeys; j += 32) {
+        if constexpr (F::kTurns) __builtin_amdgcn_s_setprio(1);
         const f32x16 dp = gradients(vt, j);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
+          if constexpr (F::kTurns) __builtin_amdgcn_s_setprio(1);
           f32x16 s = scores(kt, key, j, m, masked);
+          if constexpr (F::kTurns) __builtin_amdgcn_s_setprio(2);
           float part = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -198,9 +205,8 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
             s[i] = p * (dp[i] - mean[m]);
           }
           if (m) dl += part;
-          // the softmax of a single key does not move (its row sum is exact here)
-          if (masked && limit <= 1) s = f32x16{};
           const Frag<T> lo = pack<T>(s, 0), hi = pack<T>(s, 8);
+          if constexpr (F::kTurns) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
           for (int t = 0; t < D / 32; ++t) {
             acc[m][t] = Mma<T>::run(KV::across(kc, j, m * D + t * 32), lo, acc[m][t]);
@@ -217,6 +223,13 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
     if (begin == 0 && end <= 0) a.rowstat[stat] = a.rowstat[map + stat] = 0.f;
   }
   if (!a.dq) return;
+  // the softmax of a single key does not move
+  if (limit <= 1) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) acc[m][t] = f32x16{};
+  }
   if constexpr (SPLIT) {
     float *p = a.part + (split * map + (static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;
 #pragma unroll
