@@ -227,7 +227,7 @@ __device__ __forceinline__ Frag<T> pack(const f32x16 &v, int from) {
 
 // acc += a chain of N products whose first operands, read(i), come from LDS up to
 // four products ahead of their use; second(i) is at hand.  (Left to itself the
-// compiler reads, waits and multiplies.  dk/dv has no registers for it: there it
+// compiler reads, waits and multiplies.  dk/dv has no registers for it beyond d = 32: there it
 // spilled and cost 3%.)
 template <typename T, int N, typename R, typename S>
 __device__ __forceinline__ f32x16 chain(R read, S second, f32x16 acc) {

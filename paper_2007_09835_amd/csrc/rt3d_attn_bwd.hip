@@ -301,6 +301,10 @@ struct Dkv {
   // otherwise keys wait in LDS.  32-bit values of 256 columns (and their keys)
   // pass both: they are read again for every tile, from L1.
   static constexpr bool kHoldV = sizeof(T) == 2 || D <= 64, kHoldK = D <= 32, kLdsK = !kHoldK && kHoldV;
+  // Operands read ahead of their products and waves that take turns, as in dq, where
+  // registers are left for it: up to d = 32 in 16 bits.  (4 clips of 4096 tokens, 4
+  // heads, d 32: 256 us without, 225.  At d 64 it spilled and cost 3%.)
+  static constexpr bool kAhead = sizeof(T) == 2 && kHoldK;
   // Beyond d = 64 both gradients (2 x 32 x 256 results) would take every
   // accumulator and leave none for scores: the kernel runs once for each.
   static constexpr bool kApart = D > 64;
@@ -437,7 +441,10 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
       const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
       f32x16 dp = {}, pv;
-      if constexpr (DK) {
+      if constexpr (F::kAhead) {
+        __builtin_amdgcn_s_setprio(1);
+        dp = chain<T, 2 * D / 16>([&](int i) { return Q::along(gt, 0, i * 16); }, [&](int i) { return vf[i]; }, dp);
+      } else if constexpr (DK) {
 #pragma unroll
         for (int i = 0; i < 2 * D / 16; ++i) {
           Frag<T> b;
@@ -450,15 +457,28 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         f32x16 s = {};
+        Frag<T> qn[2][D / 32];  // queries of dk's products, on their way during the probabilities
+        if constexpr (F::kAhead) {
+          __builtin_amdgcn_s_setprio(1);
+          s = chain<T, D / 16>([&](int i) { return Q::along(qt, 0, m * D + i * 16); },
+                               [&](int i) { return kf[m][i]; }, s);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          Frag<T> b;
-          if constexpr (F::kHoldK) b = kf[m][i];
-          else if constexpr (F::kLdsK) b = F::K::along(kt, 0, m * D + i * 16);
-          else b = key_frag(m, i);
-          s = Mma<T>::run(Q::along(qt, 0, m * D + i * 16), b, s);
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) qn[h][c] = Q::across(qc, 16 * h, m * D + c * 32);
+          __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_s_setprio(2);
+        } else {
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            Frag<T> b;
+            if constexpr (F::kHoldK) b = kf[m][i];
+            else if constexpr (F::kLdsK) b = F::K::along(kt, 0, m * D + i * 16);
+            else b = key_frag(m, i);
+            s = Mma<T>::run(Q::along(qt, 0, m * D + i * 16), b, s);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -488,9 +508,12 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const Frag<T> ds = pack<T>(s, 8 * h);
+          if constexpr (F::kAhead) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c)
-            dk[m][c] = Mma<T>::run(Q::across(qc, 16 * h, m * D + c * 32), ds, dk[m][c]);
+          for (int c = 0; c < D / 32; ++c) {
+            if constexpr (!F::kAhead) qn[h][c] = Q::across(qc, 16 * h, m * D + c * 32);
+            dk[m][c] = Mma<T>::run(qn[h][c], ds, dk[m][c]);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
