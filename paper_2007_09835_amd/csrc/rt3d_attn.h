@@ -293,10 +293,14 @@ __device__ __forceinline__ bool place(const AttnArgs &a, const int32_t *walk, in
   if (a.sets) {
     const unsigned sets = a.sets, pairs = static_cast<unsigned>(a.n) * a.hk / sets, set = id % sets;
     id /= sets;
-    p.split = static_cast<int>(id % splits);
+    const unsigned split = id % splits;
     id /= splits;
     p.rank = static_cast<int>(id / pairs);
     pair = set * pairs + id % pairs;
+    // A causal split has more work the earlier it is: the splits of neighbouring tiles
+    // change places, or those of one kind would meet on the same XCDs and CUs.  (8000
+    // tokens, 4 heads, d 64, two splits: forward 159 us, 175 without.)
+    p.split = static_cast<int>((split + __builtin_popcount(p.rank)) % splits);
   } else {
     p.split = static_cast<int>(id % splits);
     id /= splits;

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import token_refs as refs
-from paper_2007_09835_amd import build, layers
+from paper_2007_09835_amd import build, layers, rt3d
 
 pytestmark = pytest.mark.gpu
 
@@ -292,3 +292,13 @@ def test_nothing_to_do():
     o, saved = layers.diff_attention(q, k, v, lam, save=True)
     dq, dk, dv, dl = layers.diff_attention_backward(o, q, k, v, lam, saved)
     assert not dk.any() and not dv.any() and not dl.any()
+
+
+@pytest.mark.parametrize("n, l, hk, group, d, frame, dtype", [
+    (1, 1500, 4, 1, 64, 49, "bf16"), (1, 1100, 1, 3, 32, 1, "f16"), (2, 900, 3, 1, 40, 100, "bf16"),
+    (1, 700, 2, 2, 128, 49, "f16"), (1, 600, 5, 1, 32, 1, "f32")])
+def test_causal_calls_that_split(n, l, hk, group, d, frame, dtype):
+    """Causal walks in three and more splits, whose order changes from tile to tile."""
+    desc = rt3d.make_diffattn_desc(n, l, l, hk * group, hk, d, dtype, frame)
+    assert rt3d.rt3d_diffattn_fwd_workspace_size(desc) > 0
+    _check(71, n, l, l, hk * group, hk, d, dtype, frame=frame)
