@@ -227,7 +227,7 @@ __device__ __forceinline__ Frag<T> pack(const f32x16 &v, int from) {
 
 // acc += a chain of N products whose first operands, read(i), come from LDS up to
 // four products ahead of their use; second(i) is at hand.  (Left to itself the
-// compiler reads, waits and multiplies.  dk/dv has no registers for it beyond d = 32: there it
+// compiler reads, waits and multiplies.  dk/dv has no registers for it at d = 64: there it
 // spilled and cost 3%.)
 template <typename T, int N, typename R, typename S>
 __device__ __forceinline__ f32x16 chain(R read, S second, f32x16 acc) {
@@ -240,6 +240,23 @@ __device__ __forceinline__ f32x16 chain(R read, S second, f32x16 acc) {
   for (int i = 0; i < N; ++i) {
     acc = Mma<T>::run(f[i % kRing], second(i), acc);
     if (i + kRing < N) f[i % kRing] = read(i + kRing);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  return acc;
+}
+
+// The same with both operands in LDS.
+template <typename T, int N, typename R, typename S>
+__device__ __forceinline__ f32x16 chain_both(R read, S second, f32x16 acc) {
+  constexpr int kRing = N < 4 ? N : 4;
+  Frag<T> f[kRing], g[kRing];
+#pragma unroll
+  for (int i = 0; i < kRing; ++i) f[i] = read(i), g[i] = second(i);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    acc = Mma<T>::run(f[i % kRing], g[i % kRing], acc);
+    if (i + kRing < N) f[i % kRing] = read(i + kRing), g[i % kRing] = second(i + kRing);
     __builtin_amdgcn_sched_barrier(0);
   }
   return acc;

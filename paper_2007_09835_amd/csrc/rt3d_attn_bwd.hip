@@ -302,9 +302,10 @@ struct Dkv {
   // pass both: they are read again for every tile, from L1.
   static constexpr bool kHoldV = sizeof(T) == 2 || D <= 64, kHoldK = D <= 32, kLdsK = !kHoldK && kHoldV;
   // Operands read ahead of their products and waves that take turns, as in dq, where
-  // registers are left for it: up to d = 32 in 16 bits.  (4 clips of 4096 tokens, 4
-  // heads, d 32: 256 us without, 225.  At d 64 it spilled and cost 3%.)
-  static constexpr bool kAhead = sizeof(T) == 2 && kHoldK;
+  // registers are left for it: in 16 bits, but not with both gradients at d = 64.  (4
+  // clips of 4096 tokens, 4 heads, d 32: 256 us without, 225; 2 clips, 8 heads, d 128: dk
+  // 783 and 724, dv 574 and 541.  At d 64 it spilled and cost 3%.)
+  static constexpr bool kAhead = sizeof(T) == 2 && (D <= 32 || D > 64);
   // Beyond d = 64 both gradients (2 x 32 x 256 results) would take every
   // accumulator and leave none for scores: the kernel runs once for each.
   static constexpr bool kApart = D > 64;
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
       const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
       f32x16 dp = {}, pv;
-      if constexpr (F::kAhead) {
+      if constexpr (F::kAhead && DK) {
         __builtin_amdgcn_s_setprio(1);
         dp = chain<T, 2 * D / 16>([&](int i) { return Q::along(gt, 0, i * 16); }, [&](int i) { return vf[i]; }, dp);
       } else if constexpr (DK) {
@@ -460,10 +461,11 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
         Frag<T> qn[2][D / 32];  // queries of dk's products, on their way during the probabilities
         if constexpr (F::kAhead) {
           __builtin_amdgcn_s_setprio(1);
-          s = chain<T, D / 16>([&](int i) { return Q::along(qt, 0, m * D + i * 16); },
-                               [&](int i) { return kf[m][i]; }, s);
+          auto queries = [&](int i) { return Q::along(qt, 0, m * D + i * 16); };
+          if constexpr (F::kHoldK) s = chain<T, D / 16>(queries, [&](int i) { return kf[m][i]; }, s);
+          else s = chain_both<T, D / 16>(queries, [&](int i) { return F::K::along(kt, 0, m * D + i * 16); }, s);
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int h = 0; DK && h < 2; ++h)
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) qn[h][c] = Q::across(qc, 16 * h, m * D + c * 32);
           __builtin_amdgcn_sched_barrier(0);
