@@ -471,7 +471,7 @@ rt3d_status rt3d_rope3d(const rt3d_rope_desc *desc, const void *x, const int32_t
  * those of the query's own frame and of earlier ones, where a frame is `frame`
  * tokens (1: ordinary causal attention) and the queries end where the keys end:
  * query i of q_len stands at key position k_len - q_len + i.  A query that sees
- * no key gives zeros. */
+ * no key gives zeros, and so does one map of it whose scores are all -inf. */
 typedef struct {
     int32_t n, lq, lk;        /* clips, queries and keys of a (padded) clip */
     int32_t hq, hk;           /* query and key heads, hq a multiple of hk */
@@ -498,7 +498,8 @@ rt3d_status rt3d_diffattn_fwd_workspace_size(const rt3d_diffattn_desc *desc, uin
  * the others of their tile: a value there must be finite (as zero times it is added),
  * and for the backward pass so must keys, queries and output gradients.  o2 and lse are what the backward pass needs, or NULL: o2 the second
  * map's output P_2 v, tight [n][lq][hq][2 d] in desc->dtype, lse float32
- * [2][n][hq][lq], the base-2 logarithm of each map's softmax denominator.
+ * [2][n][hq][lq], the base-2 logarithm of each map's softmax denominator (+inf for
+ * a map of zeros).
  * Pointers must be 16-byte aligned (lambda, lse and lengths 4), pitches and batch
  * strides multiples of 16 bytes; a pitch is below 2^22 elements, lq * (hq / hk), lk
  * and frame below 2^30.  n = 0 or lq = 0: nothing is read or written.  o and o2

@@ -43,10 +43,11 @@ struct Fwd {
   static_assert(kMaps == 2 || ROWS * 32 * kWidth * 4 <= kLds, "the second maps' results fit");
 };
 
-// A row's reference is the maximum of its first 32 keys, and no maximum is formed
-// after that: a step whose probabilities against the reference add up to more than
-// this (in a lane, 16 keys) is done again with a new one, everything before it scaled
-// down.  P up to 2^8 fits every type, and steps after the first hardly ever get there.
+// A row's reference is the maximum of its first 32 keys (or of the first 32 that hold
+// a score above -inf), and no maximum is formed after that: a step whose probabilities
+// against the reference add up to more than this (in a lane, 16 keys) is done again
+// with a new one, everything before it scaled down.  P up to 2^8 fits every type, and
+// steps after the first hardly ever get there.
 constexpr float kMost = 256.f;
 
 template <typename T, int D, int ROWS, bool SPLIT>
@@ -126,13 +127,15 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
         for (int i = 0; i < 16; ++i)
           if (key + result_row(i, half) >= limit) s[m][i] = -INFINITY;
     };
-    auto raise = [&](const Scores &s) {  // the reference, to the maximum so far
+    // the reference, to the maximum so far (found: of rows that have one already, too)
+    auto raise = [&](const Scores &s, bool found) {
 #pragma unroll
       for (int m = 0; m < kMaps; ++m) {
         float most = s[m][0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) most = fmaxf(most, s[m][i]);
-        const float now = fmaxf(top[m], half_max(most) * a.scale2);
+        const float seen = half_max(most) * a.scale2;
+        const float now = found || top[m] == -INFINITY ? fmaxf(top[m], seen) : top[m];
         const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
         top[m] = now;
         sum[m] *= by;
@@ -159,6 +162,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
     };
     stage(begin, 0);
     int buf = 0;
+    bool start = true;  // some row of this wave has no reference yet
     for (int tile_key = begin; tile_key < end; tile_key += kKeys, buf ^= 1) {
       tile_barrier();  // this tile has landed, and the other buffer is read
       const unsigned kt = KV::at(k_lane, lds + buf * 2 * KV::kBytes), vt = KV::at(v_lane, lds + (buf * 2 + 1) * KV::kBytes);
@@ -199,16 +203,27 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
         if (F::kLate && j == 0 && more) stage(tile_key + kKeys, buf ^ 1);
         if (key + 32 > whole) hide(s, key);
         if constexpr (F::kTurns) __builtin_amdgcn_s_setprio(2);
-        const bool start = key == begin;
-        if (start) raise(s);
+        const bool raised = start;
+        if (raised) {
+          raise(s, false);
+          bool open = false;
+#pragma unroll
+          for (int m = 0; m < kMaps; ++m) {
+            float all = s[m][0];  // -inf, or NaN: a row of NaN finds none and needs none
+#pragma unroll
+            for (int i = 1; i < 16; ++i) all += s[m][i];
+            open |= top[m] == -INFINITY && all == -INFINITY;
+          }
+          start = __any(open && in && limit > begin);
+        }
         float part[kMaps];
         bool over = probabilities(s, part);
-        if (__builtin_expect(!start && __any(over), 0)) {
+        if (__builtin_expect(!raised && __any(over), 0)) {
 #pragma unroll
           for (int m = 0; m < kMaps; ++m) s[m] = f32x16{};
           scores(s, kt, j);
           if (key + 32 > whole) hide(s, key);
-          raise(s);
+          raise(s, true);
           probabilities(s, part);
         }
 #pragma unroll
@@ -267,17 +282,18 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
     return;
   }
 
-  // A row that sees no key, and rows behind the clip's end: zeros, and a
-  // logarithm of +inf, which makes every probability of the backward pass zero.
-  // (A sum of NaN is not zero: it goes into the row's results.)
-  const bool any = in && sum[0] != 0.f;
+  // A map of a row that sees no key (or none with a score above -inf), and rows behind
+  // the clip's end: zeros, and a logarithm of +inf, which makes every probability of
+  // the backward pass zero.  (A sum of NaN is not zero: it goes into the row's results.)
+  bool any[kMaps];
 #pragma unroll
   for (int m = 0; m < kMaps; ++m) {
-    const float inv = any ? 1.f / sum[m] : 0.f;
+    any[m] = in && sum[m] != 0.f;
+    const float inv = any[m] ? 1.f / sum[m] : 0.f;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[m][t][i] = any ? acc[m][t][i] * inv : 0.f;
+      for (int i = 0; i < 16; ++i) acc[m][t][i] = any[m] ? acc[m][t][i] * inv : 0.f;
   }
   const float *handed = reinterpret_cast<const float *>(smem) + (wave >> 1) * 32 * F::kWidth + lane;
   if constexpr (kMaps == 1) {
@@ -320,7 +336,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
     const int64_t stat = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
 #pragma unroll
     for (int m = 0; m < kMaps; ++m)
-      a.lse[(map0 + m) * static_cast<int64_t>(a.n) * a.hq * a.lq + stat] = any ? top[m] + log2f(sum[m]) : INFINITY;
+      a.lse[(map0 + m) * static_cast<int64_t>(a.n) * a.hq * a.lq + stat] = any[m] ? top[m] + log2f(sum[m]) : INFINITY;
   }
 }
 
@@ -368,11 +384,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   for (int w = 32; w > 0; w >>= 1)
 #pragma unroll
     for (int m = 0; m < 2; ++m) sum[m] += __shfl_xor(sum[m], w, 64);
-  const bool any = in && sum[0] != 0.f;
   const float lam = a.lam[head];
   T *o = static_cast<T *>(a.out) + clip * a.o_batch + query * a.o_pitch + static_cast<int64_t>(head) * 2 * a.d;
   T *o2 = static_cast<T *>(a.out2) + ((static_cast<int64_t>(clip) * a.lq + query) * a.hq + head) * 2 * a.d;
   const int m = lane >> 5;
+  const float total_sum = m ? sum[1] : sum[0], total_top = m ? top[1] : top[0];
+  const bool any = in && total_sum != 0.f;
   const float *part = a.part + a.splits * total * 4 + r * 4 * a.d + m * 2 * a.d;
   const int64_t step = total * 4 * a.d;
   struct alignas(4 * sizeof(T)) Four {
@@ -381,7 +398,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   for (int c0 = 0; c0 < 2 * a.d; c0 += 128) {
     const int col = c0 + (lane & 31) * 4;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (any) {
+    if (in) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int n = min(64, a.splits - i * 64);
@@ -417,7 +434,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     Four x, y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float mine = any ? v[e] / sum[m] : 0.f, other = __shfl_xor(mine, 32, 64);
+      const float mine = any ? v[e] / total_sum : 0.f, other = __shfl_xor(mine, 32, 64);
       x.v[e] = static_cast<T>(mine - lam * other);
       y.v[e] = static_cast<T>(mine);
     }
@@ -427,7 +444,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   }
   if (a.lse && share == 0 && (lane & 31) == 0) {
     const int64_t at = (static_cast<int64_t>(clip) * a.hq + head) * a.lq + query;
-    a.lse[m * static_cast<int64_t>(a.n) * a.hq * a.lq + at] = any ? top[m] + log2f(sum[m]) : INFINITY;
+    a.lse[m * static_cast<int64_t>(a.n) * a.hq * a.lq + at] = any ? total_top + log2f(total_sum) : INFINITY;
   }
 }
 
