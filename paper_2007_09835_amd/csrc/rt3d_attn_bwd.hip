@@ -155,29 +155,35 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
       return s;
     };
     stage(begin, 0);
-    // Few keys: the roundings of o and of the probabilities in it do not average
-    // out, and a row sum formed from o is as far off as the differences dP - A are
-    // small (two keys: up to 0.43% of dq and dk in bf16). One tile more of work
-    // sums P dP itself.
-    if (!SPLIT && end <= kKeys) {
+    // Rows of few keys, all of them in the first tile: the roundings of o and of the
+    // probabilities in it do not average out, and a row sum formed from o is as far off
+    // as the differences dP - A are small (bf16, d 64, two keys, normal inputs: dq is
+    // 0.45% off in the median and 6% in one row of twenty, with values around 3 1.3% and
+    // 21%; with exact sums 0.2% and 0.35%). One tile more of work sums P dP itself,
+    // whatever the workgroup's other rows see.
+    const int first_block = visible(tile * WAVES * 32 / a.group, q_len, k_len, a.frame);
+    if (begin == 0 && first_block <= kKeys) {
       tile_barrier();
       const unsigned kt = KV::at(along, lds), vt = KV::at(along, lds + KV::kBytes);
-      mean[0] = mean[1] = 0.f;
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < kKeys; j += 32) {
-        if (j >= wave_end) break;
+        if (j >= wave_end || whole > kKeys) break;
         const f32x16 dp = gradients(vt, j);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
           const f32x16 s = scores(kt, 0, j, m, true);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) mean[m] += __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -lse[m])) * dp[i];
+          for (int i = 0; i < 16; ++i) sum[m] += __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -lse[m])) * dp[i];
         }
       }
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        mean[m] = half_sum(mean[m]);
-        if (in && half == 0) a.rowstat[m * map + stat] = mean[m];
+        sum[m] = half_sum(sum[m]);
+        if (limit <= kKeys) {
+          mean[m] = sum[m];
+          if (half == 0) a.rowstat[m * map + stat] = mean[m];
+        }
       }
     }
     int buf = 0;
