@@ -47,7 +47,10 @@ struct Fwd {
 // a score above -inf), and no maximum is formed after that: a step whose probabilities
 // against the reference add up to more than this (in a lane, 16 keys) is done again
 // with a new one, everything before it scaled down.  P up to 2^8 fits every type, and
-// steps after the first hardly ever get there.
+// steps after the first hardly ever get there where scores are alike along the keys.
+// (8 clips of 4096 tokens, 8 heads, d 64: 705 us; scores that rise by 10 along the
+// clip 746, by 160 932; a rise that repeats every step 1254.  8 clips of 1568, d 32: 95,
+// 112, 163, 166.)
 constexpr float kMost = 256.f;
 
 template <typename T, int D, int ROWS, bool SPLIT>

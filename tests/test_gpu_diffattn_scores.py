@@ -134,3 +134,20 @@ def test_gradients_where_scores_pass_the_range(d, dtype, lq, lk):
             assert not got[:, :37].any()
             got = got[:, 37:]
         refs.within(got, ref[name], ref[name + "_err"] + half * ref[name].abs() + tiny, name)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (64, "f16"), (128, "bf16"), (128, "f16"), (64, "f32"), (96, "f32")])
+@pytest.mark.parametrize("lq,lk", [(33, 700), (200, 300), (1, 3000)])
+def test_scores_that_rise_along_the_keys(d, dtype, lq, lk):
+    """One map's scores rise by 160 over the keys, so that every second step of 32 or
+    so starts again with a new reference; the other's fall.  Beyond d 32, where the
+    values' loads and the maps are dealt out otherwise."""
+    q, k, v, _, lam = _inputs(31, 1, lq, lk, 1, 1, d, dtype)
+    ramp = torch.linspace(0, 20, lk)
+    for m, by in ((0, ramp), (1, -ramp)):
+        kk, qq = k[0], q[0]
+        kk[0, :, 0, m, 0], qq[0, :, 0, m, 0] = by.to(kk.dtype), 8.0
+    for t in (q, k):
+        t[1].copy_(t[0].double())
+    none = torch.zeros(lk, dtype=torch.bool)
+    _forward_check(q, k, v, lam, (none, none), dtype, scale=1.0, far=512.0)
