@@ -202,27 +202,46 @@ double walk_share(const rt3d_diffattn_desc *d) {
   if (!d->frame || d->frame >= d->lk) return 1.0;
   return d->lq <= d->lk ? 1.0 - 0.5 * d->lq / d->lk : 0.5 * d->lk / d->lq;
 }
+// `part(s)`: the steps of a walk that is asked for s splits, and how many that makes.
+// At most `most` splits are made (and asked for at most `tries`).
+template <typename Part>
 int pick_splits(const rt3d_diffattn_desc *d, int64_t blocks, int64_t steps, double step_us, double part_bytes,
-                int64_t most) {
+                int64_t tries, int64_t most, Part &&part) {
   const double share = walk_share(d);
   if (blocks <= 0 || blocks * share >= 2 * kCus || steps < 2) return 1;
   const double shared = d->dtype == RT3D_F32 ? 1.0 : 0.6;
-  auto time = [&](int64_t s) {
+  auto time = [&](int64_t walk, int64_t s) {
     const double on_cu = share * static_cast<double>((blocks * s + kCus - 1) / kCus);
-    const double walk = static_cast<double>((steps + s - 1) / s) * step_us;
-    return walk * std::max(1.0, shared * on_cu) + (s > 1 ? 5.0 + 2 * s * part_bytes / 4e6 : 0.0);
+    return walk * step_us * std::max(1.0, shared * on_cu) + (s > 1 ? 5.0 + 2 * s * part_bytes / 4e6 : 0.0);
   };
   int best = 1;
-  double least = time(1);
-  for (int64_t s = 2; s <= most && s <= steps; ++s) {
-    const double t = time(s);
-    if (t < least) least = t, best = static_cast<int>(s);
+  double least = time(steps, 1);
+  for (int64_t s = 2; s <= tries && s <= steps; ++s) {
+    const auto [walk, made] = part(s);
+    if (made < 2 || made > most) continue;
+    const double t = time(walk, made);
+    if (t < least) least = t, best = static_cast<int>(made);
   }
   return best;
 }
 
-// Keys of a split: whole staged tiles (of 32 or 64 keys), so that none reaches into the next.
-int split_span(int lk, int splits) { return static_cast<int>((static_cast<int64_t>(lk) + splits - 1) / splits + 63) / 64 * 64; }
+// Keys of a split: whole staged tiles (of 32 or 64 keys), so that none reaches into
+// the next.  That makes split_count splits, often fewer than asked for; asked for so
+// many, the span is the same.  Plans are made of these counts, so that the workspace of
+// one pays for it again.
+int split_span(int lk, int64_t splits) { return static_cast<int>((lk + splits - 1) / splits + 63) / 64 * 64; }
+int split_count(int lk, int span) { return static_cast<int>((static_cast<int64_t>(lk) + span - 1) / span); }
+
+struct Walk {
+  int64_t steps, splits;
+};
+int pick_key_splits(const rt3d_diffattn_desc *d, int64_t blocks, double step_us, double part_bytes, int64_t tries,
+                    int64_t most) {
+  return pick_splits(d, blocks, (d->lk + 31) / 32, step_us, part_bytes, tries, most, [&](int64_t s) {
+    const int span = split_span(d->lk, s);
+    return Walk{span / 32, split_count(d->lk, span)};
+  });
+}
 
 // Time of a step of 32 keys (forward, dq) or 32 queries (dk, dv) of a workgroup
 // alone on its CU, in us per 32 channels of d: 32-bit steps take their products
@@ -251,17 +270,18 @@ FwdPlan fwd_plan(const rt3d_diffattn_desc *d, const Shape &s, uint64_t workspace
   p.span = d->lk;
   const uint64_t one = static_cast<uint64_t>(pairs * rows) * (4 + 4 * d->d) * sizeof(float);
   if (p.blocks <= 0) return p;
-  const int64_t most = std::min<int64_t>(256, static_cast<int64_t>(workspace / one));
+  constexpr int64_t kMost = 256;
+  const int64_t most = std::min<int64_t>(kMost, static_cast<int64_t>(workspace / one));
   int64_t splits;
   if (p.row_groups == 1) {
     // bound by the cache's bytes: enough waves to keep them coming
     splits = std::min<int64_t>({most, kSplitBlocks / p.blocks, d->lk / kSplitKeys});
   } else {
-    splits = pick_splits(d, p.blocks, (d->lk + 31) / 32, step_us(d, 0.35, 2.9), static_cast<double>(one), most);
+    splits = pick_key_splits(d, p.blocks, step_us(d, 0.35, 2.9), static_cast<double>(one), kMost, most);
   }
   if (splits > 1) {
-    p.span = split_span(d->lk, static_cast<int>(splits));
-    p.splits = (d->lk + p.span - 1) / p.span;
+    p.span = split_span(d->lk, splits);
+    p.splits = split_count(d->lk, p.span);
   }
   if (p.splits > 1) {
     p.blocks *= p.splits;
@@ -276,15 +296,11 @@ BwdPlan bwd_plan(const rt3d_diffattn_desc *d, const Shape &s) {
   const uint64_t stats = static_cast<uint64_t>(d->n) * d->hq * d->lq;
   const uint64_t dq = stats * 2 * d->d, dkv = static_cast<uint64_t>(pairs) * d->lk * 4 * d->d;
   p.dq_span = d->lk;
-  p.dq_splits = pick_splits(d, pairs * ((rows + kBwdRows - 1) / kBwdRows), (d->lk + 31) / 32,
-                            step_us(d, 0.35, 2.9), dq * 4.0, 16);
-  if (p.dq_splits > 1) {
-    p.dq_span = split_span(d->lk, p.dq_splits);
-    p.dq_splits = (d->lk + p.dq_span - 1) / p.dq_span;
-  }
-  p.dkv_splits = pick_splits(d, pairs * ((d->lk + kBwdRows - 1) / kBwdRows),
-                             static_cast<int64_t>(s.group) * ((d->lq + 31) / 32), step_us(d, 0.45, 3.9),
-                             dkv * 4.0, 16);
+  p.dq_splits = pick_key_splits(d, pairs * ((rows + kBwdRows - 1) / kBwdRows), step_us(d, 0.35, 2.9), dq * 4.0, 16, 16);
+  if (p.dq_splits > 1) p.dq_span = split_span(d->lk, p.dq_splits);
+  const int64_t tiles = static_cast<int64_t>(s.group) * ((d->lq + 31) / 32);
+  p.dkv_splits = pick_splits(d, pairs * ((d->lk + kBwdRows - 1) / kBwdRows), tiles, step_us(d, 0.45, 3.9), dkv * 4.0,
+                             16, 16, [&](int64_t s) { return Walk{(tiles + s - 1) / s, s}; });
   auto up = [](uint64_t floats) { return (floats + 3) / 4 * 4; };  // parts begin at 16 bytes
   p.dq_part = up((2 + p.dq_splits) * stats);
   p.dkv_part = p.dq_part + (p.dq_splits > 1 ? up(p.dq_splits * dq) : 0);
