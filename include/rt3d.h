@@ -390,6 +390,8 @@ rt3d_status rt3d_group_reweight(const rt3d_group_desc *desc, const void *w, cons
  * need only the alignment of an element (16-byte aligned pointers and pitches
  * of whole 16 bytes are faster).  Sums, statistics and softmax are float32 with a
  * fixed order: repeated calls give identical results.  Calls may be captured.
+ * A call that would need a launch of 2^32 threads or more is refused
+ * (RT3D_ERR_UNSUPPORTED) before anything of it is started.
  * ------------------------------------------------------------------------ */
 
 /* Layout of a batch of token rows: elements between neighbouring tokens of a

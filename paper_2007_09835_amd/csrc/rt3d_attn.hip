@@ -454,6 +454,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 template <typename T, int D, int ROWS, bool SPLIT>
 int fwd(const AttnArgs &a, hipStream_t s) {
   using F = Fwd<T, D, ROWS>;
+  static_assert(F::kThreads == attn_fwd_threads(D, ROWS), "what the host checks the launch for");
   const int e = allow_lds<attn_fwd_kernel<T, D, ROWS, SPLIT>>(F::kLds);
   if (e != hipSuccess) return e;
   attn_fwd_kernel<T, D, ROWS, SPLIT><<<grid_of(a.blocks), F::kThreads, F::kLds, s>>>(a);

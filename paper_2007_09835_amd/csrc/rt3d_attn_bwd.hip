@@ -672,7 +672,7 @@ int launch_keys(const AttnArgs &a, hipStream_t s) {
   using F = Dkv<T, D, kWaves>;
   const int e = allow_lds<attn_dkv_kernel<T, D, kWaves, SPLIT, DK, DV>>(F::kLds);
   if (e != hipSuccess) return e;
-  static_assert(F::kThreads == 256, "sum_dlam's workgroup");
+  static_assert(F::kThreads == 256 && F::kThreads == kBwdThreads, "sum_dlam's workgroup, and what the host checks");
   attn_dkv_kernel<T, D, kWaves, SPLIT, DK, DV><<<grid_of(a.blocks) + a.dlam_blocks, F::kThreads, F::kLds, s>>>(a);
   return hipGetLastError();
 }

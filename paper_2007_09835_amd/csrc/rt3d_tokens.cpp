@@ -12,7 +12,7 @@
 namespace rt3d {
 namespace {
 
-constexpr int64_t kMaxBlocks = (1ll << 31) - 16;
+constexpr int64_t kMaxRows = (1ll << 31) - 16;
 constexpr int kMaxNormColumns = 1 << 20;
 constexpr int64_t kMaxPitch = 1 << 22;   // elements: a tile's rows stay within 2^31 bytes
 constexpr int kMaxLength = 1 << 30;
@@ -22,6 +22,13 @@ constexpr int kSplitKeys = 256;      // least keys of such a split
 bool known_dtype(int dtype) { return dtype == RT3D_F32 || dtype == RT3D_BF16 || dtype == RT3D_F16; }
 int esize(int dtype) { return dtype == RT3D_F32 ? 4 : 2; }
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// A launch has fewer than 2^32 threads along its grid: HIP takes no more.
+rt3d_status check_launch(int64_t workgroups, int threads, const char *what) {
+  if (workgroups >= ((1ll << 32) + threads - 1) / threads)
+    return fail(RT3D_ERR_UNSUPPORTED, "too many %s for one call: a launch of 2^32 threads", what);
+  return RT3D_OK;
+}
 
 rt3d_status launched(int e) {
   if (e != hipSuccess)
@@ -129,7 +136,7 @@ rt3d_status check_attn(const rt3d_diffattn_desc *d, bool backward, Shape &s) {
       static_cast<int64_t>(d->lq) * s.group >= kMaxLength)
     return fail(RT3D_ERR_UNSUPPORTED, "lengths (times hq / hk) must be below 2^30");
   const double rows = static_cast<double>(d->n) * d->hk * (static_cast<double>(d->lq) * s.group + d->lk + 64);
-  if (rows >= static_cast<double>(kMaxBlocks)) return fail(RT3D_ERR_UNSUPPORTED, "more than 2^31 rows");
+  if (rows >= static_cast<double>(kMaxRows)) return fail(RT3D_ERR_UNSUPPORTED, "more than 2^31 rows");
   s.q_row = 2ll * d->hq * d->d;
   s.k_row = 2ll * d->hk * d->d;
   const int es = esize(d->dtype);
@@ -308,6 +315,26 @@ BwdPlan bwd_plan(const rt3d_diffattn_desc *d, const Shape &s) {
   return p;
 }
 
+// Whether every launch of a call can be made (workgroups go round eight XCDs).
+int64_t by_eight(int64_t workgroups) { return (workgroups + 7) / 8 * 8; }
+
+rt3d_status check_fwd_launches(const rt3d_diffattn_desc *d, const FwdPlan &p) {
+  rt3d_status st = check_launch(by_eight(p.blocks), attn_fwd_threads(d->d, p.row_groups), "rows");
+  if (st == RT3D_OK && p.splits > 1) st = check_launch(static_cast<int64_t>(d->n) * d->hq * d->lq, 256, "rows");
+  return st;
+}
+
+rt3d_status check_bwd_launches(const rt3d_diffattn_desc *d, const Shape &s, const BwdPlan &p) {
+  const int64_t rows = static_cast<int64_t>(d->lq) * s.group, pairs = static_cast<int64_t>(d->n) * d->hk;
+  auto tiles = [](int64_t len) { return (len + kBwdRows - 1) / kBwdRows; };
+  rt3d_status st = check_launch(by_eight(pairs * tiles(rows) * p.dq_splits), kBwdThreads, "queries");
+  if (st == RT3D_OK) st = check_launch(by_eight(pairs * tiles(d->lk) * p.dkv_splits) + d->hq, kBwdThreads, "keys");
+  // the sums of the splits' gradients
+  if (st == RT3D_OK && p.dq_splits > 1) st = check_launch((pairs * rows * d->d / 2 + 255) / 256, 256, "queries");
+  if (st == RT3D_OK && p.dkv_splits > 1) st = check_launch((pairs * d->lk * d->d + 255) / 256, 256, "keys");
+  return st;
+}
+
 }  // namespace
 }  // namespace rt3d
 
@@ -420,7 +447,8 @@ rt3d_status rt3d_rope3d(const rt3d_rope_desc *d, const void *x, const int32_t *p
   constexpr int64_t kThreads = 512 * 1024;  // two waves of threads for every SIMD's eight
   a.chunks = static_cast<int>(std::min<int64_t>(d->vecs, std::max<int64_t>(1, (kThreads + base - 1) / base)));
   a.threads = base * a.chunks;
-  if ((a.threads + 255) / 256 >= kMaxBlocks) return fail(RT3D_ERR_UNSUPPORTED, "too many vectors for one call");
+  const rt3d_status can = check_launch((a.threads + 255) / 256, 256, "vectors");
+  if (can != RT3D_OK) return can;
   return launched(launch_rope(a, d->dtype, halves, pairs, stream));
 }
 
@@ -429,7 +457,10 @@ rt3d_status rt3d_diffattn_fwd_workspace_size(const rt3d_diffattn_desc *d, uint64
   const rt3d_status st = check_attn(d, false, s);
   if (st != RT3D_OK) return st;
   if (!bytes) return fail(RT3D_ERR_INVALID_ARG, "bytes must be non-NULL");
-  *bytes = fwd_plan(d, s, ~0ull).bytes;
+  const FwdPlan p = fwd_plan(d, s, ~0ull);
+  const rt3d_status fits = check_fwd_launches(d, p);
+  if (fits != RT3D_OK) return fits;
+  *bytes = p.bytes;
   return ok();
 }
 
@@ -448,7 +479,8 @@ rt3d_status rt3d_diffattn_fwd(const rt3d_diffattn_desc *d, const void *q, const 
   if (!aligned(lambda, 4) || !aligned(lse, 4) || !aligned(q_len, 4) || !aligned(k_len, 4))
     return fail(RT3D_ERR_INVALID_ARG, "lambda, lse and lengths must be 4-byte aligned");
   const FwdPlan p = fwd_plan(d, s, workspace ? workspace_bytes : 0);
-  if (p.blocks >= kMaxBlocks) return fail(RT3D_ERR_UNSUPPORTED, "too many rows for one call");
+  const rt3d_status fits = check_fwd_launches(d, p);
+  if (fits != RT3D_OK) return fits;
   AttnArgs a = attn_args(d, s, q_len || k_len);
   a.q = q;
   a.k = k;
@@ -472,7 +504,10 @@ rt3d_status rt3d_diffattn_bwd_workspace_size(const rt3d_diffattn_desc *d, uint64
   const rt3d_status st = check_attn(d, true, s);
   if (st != RT3D_OK) return st;
   if (!bytes) return fail(RT3D_ERR_INVALID_ARG, "bytes must be non-NULL");
-  *bytes = bwd_plan(d, s).floats * sizeof(float);
+  const BwdPlan p = bwd_plan(d, s);
+  const rt3d_status fits = check_bwd_launches(d, s, p);
+  if (fits != RT3D_OK) return fits;
+  *bytes = p.floats * sizeof(float);
   return ok();
 }
 
@@ -494,6 +529,8 @@ rt3d_status rt3d_diffattn_bwd(const rt3d_diffattn_desc *d, const void *q, const 
   if (!aligned(lambda, 4) || !aligned(lse, 4) || !aligned(dlambda, 4) || !aligned(q_len, 4) || !aligned(k_len, 4))
     return fail(RT3D_ERR_INVALID_ARG, "lambda, dlambda, lse and lengths must be 4-byte aligned");
   const BwdPlan p = bwd_plan(d, s);
+  const rt3d_status fits = check_bwd_launches(d, s, p);
+  if (fits != RT3D_OK) return fits;
   const uint64_t need = p.floats * sizeof(float);
   if (need && (!workspace || workspace_bytes < need))
     return fail(RT3D_ERR_BUFFER_TOO_SMALL, "the backward pass needs %llu bytes of workspace, got %llu",

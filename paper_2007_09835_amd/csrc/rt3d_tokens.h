@@ -74,6 +74,7 @@ int launch_rope(const RopeArgs &a, int dtype, int halves, int pairs, void *strea
 
 // Groups of 32 rows that a workgroup of a call without splits holds, 1 or this.
 constexpr int attn_row_groups(int d) { return d > 64 ? 2 : 4; }
+constexpr int attn_fwd_threads(int d, int row_groups) { return 64 * row_groups * (d > 64 ? 2 : 1); }
 int launch_attn_fwd(const AttnArgs &a, int dtype, int row_groups, void *stream);
 
 // Splits of the backward kernels' walks (keys for dq, query tiles for dk and dv),
@@ -82,7 +83,8 @@ struct BwdPlan {
   int dq_splits, dq_span, dkv_splits;
   uint64_t dq_part, dkv_part, floats;
 };
-constexpr int kBwdRows = 128;  // rows (keys) of a backward workgroup
+constexpr int kBwdRows = 128;  // rows (keys) of a backward workgroup, 32 a wave
+constexpr int kBwdThreads = kBwdRows / 32 * 64;
 int launch_attn_bwd(const AttnArgs &a, const BwdPlan &p, int dtype, void *stream);
 
 }  // namespace rt3d
