@@ -426,6 +426,7 @@ rt3d_status rt3d_layernorm_bwd_workspace_size(const rt3d_norm_desc *desc, uint64
 /* With h = (x - mean) * rstd and g = dy * gamma:
  *   dx     = rstd * (g - mean_c(g) - h * mean_c(g * h))      (desc->dtype)
  *   dgamma = sum over rows of dy * h,  dbeta = sum over rows of dy   (float32 [c])
+ * where mean has 32 bits (h of a row is off by up to 2^-24 |mean| rstd for it).
  * dx, dgamma and dbeta may each be NULL (not computed); they must not overlap the
  * inputs or each other.  They are written, not added to; rows = 0 gives zero
  * dgamma and dbeta. */

@@ -113,9 +113,24 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float *lds) {
 
 constexpr int kNormThreads = 256;
 
+// A product that is rounded by itself, in no fma: every reader sees the same mean.
+__device__ __forceinline__ float mean_of(float sum, float inv) {
+#pragma clang fp contract(off)
+  return sum * inv;
+}
+
+// Variance about a row's mean, from the sums of the distances to a first one and of
+// their squares.  The first mean, of sums that round at the size of x, may lie a few
+// steps off: much, where the row's spread is small (a constant row of 1000 in 32 bits:
+// y = -0.02 with it).  off, the distances' own mean, is what it lacks.
+__device__ __forceinline__ float variance(const float (&s)[2], float inv, float off) {
+  const float v = s[1] * inv - off * off;
+  return v < 0.f ? 0.f : v;
+}
+
 // Layer norm, rows in registers: LPR lanes hold a row, NV vectors of V elements
 // each, so x is read once and the variance is the mean of squared distances (a
-// second pass over registers, not a difference of sums).  A workgroup walks rows
+// second pass over registers, not a difference of sums of x).  A workgroup walks rows
 // with its weights in registers.
 template <typename T, int V, int NV, int LPR>
 __global__ __launch_bounds__(kNormThreads) void layernorm_fwd_kernel(NormArgs a) {
@@ -142,27 +157,28 @@ __global__ __launch_bounds__(kNormThreads) void layernorm_fwd_kernel(NormArgs a)
 #pragma unroll
       for (int e = 0; e < V; ++e) s[0] += v[i][e];
     row_sum<LPR>(s, lds);
-    const float mean = s[0] * inv;
-    s[0] = 0.f;
+    const float mean = mean_of(s[0], inv);
+    float far[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        v[i][e] -= mean;
-        s[0] += (i * LPR + lane) * V + e < a.c ? v[i][e] * v[i][e] : 0.f;
+        v[i][e] = (i * LPR + lane) * V + e < a.c ? v[i][e] - mean : 0.f;
+        far[0] += v[i][e];
+        far[1] += v[i][e] * v[i][e];
       }
-    row_sum<LPR>(s, lds);
-    const float rstd = 1.f / sqrtf(s[0] * inv + a.eps);
+    row_sum<LPR>(far, lds);
+    const float off = mean_of(far[0], inv), rstd = 1.f / sqrtf(variance(far, inv, off) + a.eps);
     if (!in) continue;
     if (lane == 0) {
-      if (a.mean) a.mean[row] = mean;
+      if (a.mean) a.mean[row] = mean + off;
       if (a.rstd) a.rstd[row] = rstd;
     }
     T *y = static_cast<T *>(a.y) + row * a.y_pitch;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[i][e] = v[i][e] * rstd * g[i][e] + b[i][e];
+      for (int e = 0; e < V; ++e) v[i][e] = fmaf(fmaf(v[i][e], rstd, -off * rstd), g[i][e], b[i][e]);
       store_row(y, (i * LPR + lane) * V, a.c, v[i]);
     }
   }
@@ -184,17 +200,21 @@ __global__ __launch_bounds__(kNormThreads) void layernorm_fwd_long_kernel(NormAr
       for (int e = 0; e < V; ++e) s[0] += v[e];
     }
     row_sum<256>(s, lds);
-    const float mean = s[0] * inv;
-    s[0] = 0.f;
+    const float mean = mean_of(s[0], inv);
+    float far[2] = {0.f, 0.f};
     for (int col = threadIdx.x * V; col < a.c; col += kNormThreads * V) {
       load_row(x, col, a.c, v);
 #pragma unroll
-      for (int e = 0; e < V; ++e) s[0] += col + e < a.c ? (v[e] - mean) * (v[e] - mean) : 0.f;
+      for (int e = 0; e < V; ++e) {
+        const float w = col + e < a.c ? v[e] - mean : 0.f;
+        far[0] += w;
+        far[1] += w * w;
+      }
     }
-    row_sum<256>(s, lds);
-    const float rstd = 1.f / sqrtf(s[0] * inv + a.eps);
+    row_sum<256>(far, lds);
+    const float off = mean_of(far[0], inv), rstd = 1.f / sqrtf(variance(far, inv, off) + a.eps);
     if (threadIdx.x == 0) {
-      if (a.mean) a.mean[row] = mean;
+      if (a.mean) a.mean[row] = mean + off;
       if (a.rstd) a.rstd[row] = rstd;
     }
     for (int col = threadIdx.x * V; col < a.c; col += kNormThreads * V) {
@@ -203,7 +223,7 @@ __global__ __launch_bounds__(kNormThreads) void layernorm_fwd_long_kernel(NormAr
       load_weight(a.gamma, col, a.c, 1.f, g);
       load_weight(a.beta, col, a.c, 0.f, b);
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = (v[e] - mean) * rstd * g[e] + b[e];
+      for (int e = 0; e < V; ++e) v[e] = fmaf(fmaf(v[e] - mean, rstd, -off * rstd), g[e], b[e]);
       store_row(y, col, a.c, v);
     }
   }
