@@ -184,6 +184,9 @@ class S3DStack:
                 self.bufs[name] = torch.empty((batch, *shp), dtype=tdt, device=device)
         self.pool_bufs: Dict[str, torch.Tensor] = {}
         self.out_name = self.ops[-1][3]
+        # the last block's output lies behind the channels that its own convs read
+        self.out_off = max(op[5] + by_name[op[1]][0].c_in for op in self.ops
+                           if op[0] == "conv" and op[2] == self.out_name)
         self._schedule(n_streams)
 
     def _schedule(self, n_streams: int):
@@ -279,8 +282,10 @@ class TokenBlock:
         o = differential attention(q, k, v),  y = x + conv1x1x1(layer_norm per head(o)).
 
     ``heads`` query heads on ``key_heads`` key heads (default: as many) of 2 d =
-    c / heads channels.  ``causal``: a token sees its own frame and earlier ones.
-    Buffers are allocated once, so a pass can be captured in a HIP graph."""
+    c / heads channels, d a multiple of 8 up to 128.  ``causal``: a token sees its own
+    frame and earlier ones.  Buffers are allocated once, so a pass can be captured in a
+    HIP graph.  An input that is a view of wider voxels (a channel slice) is gathered
+    into the block's input buffer first: the residual of a conv is dense."""
 
     def __init__(self, c: int, thw, heads: int, key_heads: Optional[int] = None, batch: int = 1,
                  dtype: str = "bf16", causal: bool = False, depth: int = 0, tag: str = "tokens",
@@ -288,6 +293,8 @@ class TokenBlock:
         key_heads = heads if key_heads is None else key_heads
         if c % (2 * heads) or heads % key_heads:
             raise ValueError("c must be a multiple of 2 * heads, heads of key_heads")
+        if c // (2 * heads) % 8 or c // (2 * heads) > 128:
+            raise ValueError("c / (2 * heads) must be a multiple of 8 up to 128, not %d" % (c // (2 * heads)))
         self.c, self.thw, self.heads, self.key_heads, self.batch = c, tuple(thw), heads, key_heads, batch
         self.dtype = dtype
         self.d = d = c // (2 * heads)
@@ -331,7 +338,12 @@ class TokenBlock:
         """(name, fn) of every launch of a pass over ``x`` (default: the input buffer)."""
         x = self.x if x is None else x
         heads = lambda b: b.view(self.batch, self.tokens, self.heads, 2 * self.d)
-        return [
+        gather = []
+        if not x.is_contiguous():
+            layers._need(x, "x", self.x, self.x.shape, self.x.dtype)
+            gather = [("input", lambda wide=x: self.x.copy_(wide))]
+            x = self.x
+        return gather + [
             ("norm", lambda: layers.layer_norm(x, self.gamma, self.beta, out=self.normed)),
             ("qkv", lambda: self.qkv(self.normed, out=self.row)),
             ("rope", lambda: layers.rope3d(self.turned, self.thw, self.sections, out=self.turned)),
@@ -355,13 +367,20 @@ class TokenStack:
                  causal: bool = False, tag: Optional[str] = None):
         self.trunk, self.net, self.batch, self.dtype = trunk, trunk.net, trunk.batch, trunk.dtype
         self.x = trunk.x
-        last = list(trunk.bufs.values())[-1] if not hasattr(trunk, "out_name") else trunk.bufs[trunk.out_name]
-        _, t, h, w, c = last.shape
+        # the features: the last layer's channels of the buffer that it leaves
+        if hasattr(trunk, "out_name"):
+            last = trunk.bufs[trunk.out_name]
+            self.channels = slice(trunk.out_off, last.shape[-1])
+        else:
+            layer = trunk.layers[-1]
+            last = trunk.pool_bufs.get(layer.name, trunk.bufs[layer.name])
+            self.channels = slice(0, layer.c_out)
+        _, t, h, w, c = last[..., self.channels].shape
         self.blocks = [TokenBlock(c, (t, h, w), heads, key_heads, trunk.batch, trunk.dtype, causal, i,
                                   tag or trunk.net + "-tokens", last.device) for i in range(blocks)]
 
     def forward(self, x: Optional[torch.Tensor] = None) -> torch.Tensor:
-        y = self.trunk.forward(x)
+        y = self.trunk.forward(x)[..., self.channels]
         for block in self.blocks:
             y = block.forward(y)
         return y
