@@ -285,7 +285,9 @@ class TokenBlock:
     c / heads channels, d a multiple of 8 up to 128.  ``causal``: a token sees its own
     frame and earlier ones.  Buffers are allocated once, so a pass can be captured in a
     HIP graph.  An input that is a view of wider voxels (a channel slice) is gathered
-    into the block's input buffer first: the residual of a conv is dense."""
+    into the block's input buffer first: the residual of a conv is dense.  No input may
+    lie in a buffer that the pass writes (the block's own result among them: pass a copy
+    of that, or another block's)."""
 
     def __init__(self, c: int, thw, heads: int, key_heads: Optional[int] = None, batch: int = 1,
                  dtype: str = "bf16", causal: bool = False, depth: int = 0, tag: str = "tokens",
@@ -338,7 +340,11 @@ class TokenBlock:
         """(name, fn) of every launch of a pass over ``x`` (default: the input buffer)."""
         x = self.x if x is None else x
         heads = lambda b: b.view(self.batch, self.tokens, self.heads, 2 * self.d)
-        gather = []
+        gather, own = [], [self.normed, self.row, self.o, self.mixed, self.y]
+        if not x.is_contiguous():
+            own.append(self.x)
+        if x.untyped_storage().data_ptr() in {b.untyped_storage().data_ptr() for b in own}:
+            raise ValueError("x lies in a buffer that the block writes")
         if not x.is_contiguous():
             layers._need(x, "x", self.x, self.x.shape, self.x.dtype)
             gather = [("input", lambda wide=x: self.x.copy_(wide))]
