@@ -105,6 +105,8 @@ def maxpool3d(x: torch.Tensor, k, stride, dtype: str, out: Optional[torch.Tensor
 # they are.  Results are new tensors unless ``out`` is given.  A call runs on the
 # device of its tensors, on ``stream`` (a torch stream of that device) or else on
 # that device's current stream; its results and workspace belong to that stream.
+# Gradients come from the backward calls; results carry no autograd graph, so with
+# gradients enabled the forward calls refuse tensors that require one.
 # ---------------------------------------------------------------------------
 
 _CODES = {dt: name for name, dt in TORCH_DTYPES.items()}
@@ -126,6 +128,15 @@ def _need(t: Optional[torch.Tensor], name: str, like: torch.Tensor, shape, dtype
         raise ValueError("%s must be %s, not %s" % (name, dtype, t.dtype))
     if t.shape != shape:  # a torch.Size is a tuple
         raise ValueError("%s must be %s, not %s" % (name, list(shape), list(t.shape)))
+
+
+def _no_graph(*tensors) -> None:
+    """Refuses tensors whose gradient would be lost: the results carry no graph."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("a tensor requires a gradient, and the result would carry none: call under "
+                                 "torch.no_grad() and take gradients from the backward call")
 
 
 def _launch(x: torch.Tensor, stream, call):
@@ -168,6 +179,7 @@ def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None,
     for t, name in ((gamma, "gamma"), (beta, "beta")):
         _need(t, name, x, (c,), torch.float32)
     _need(out, "out", x, x.shape, x.dtype)
+    _no_graph(x, gamma, beta)
 
     def call():
         y = x.new_empty(x.shape) if out is None else out
@@ -239,6 +251,7 @@ def rope3d(x: torch.Tensor, grid: Sequence[int], sections: Sequence[int], base: 
         raise ValueError("a %s grid has not %d tokens" % (tuple(grid), tokens))
     _need(out, "out", x, x.shape, x.dtype)
     _need(pos, "pos", x, (n, tokens, 3), torch.int32)
+    _no_graph(x)
 
     def call():
         y = x.new_empty(x.shape) if out is None else out
@@ -286,6 +299,7 @@ def diff_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch
     the frames' mask hides must be finite.  With ``save`` also what
     ``diff_attention_backward`` needs."""
     desc = _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=out)
+    _no_graph(q, k, v, lam)
     n, lq, hq, _, d = q.shape
     shape = (n, lq, hq, 2 * d)
 
