@@ -278,8 +278,8 @@ def _diffattn_desc(q, k, v, lam, q_len, k_len, frame, scale, o=None, d_o=None):
     _need(k_len, "k_len", q, (n,), torch.int32)
     _need(o, "out", q, (n, lq, hq, 2 * d), q.dtype)
     _need(d_o, "do", q, (n, lq, hq, 2 * d), q.dtype)
-    if scale is not None and not scale > 0:
-        raise ValueError("scale must be > 0 (None: 1 / sqrt(d)), got %s" % scale)
+    if scale is not None and not 0 < ctypes.c_float(scale).value < float("inf"):
+        raise ValueError("scale must be > 0 and finite in 32 bits (None: 1 / sqrt(d)), got %s" % scale)
     row_q, row_k = hq * 2 * d, hk * 2 * d
     return rt3d.make_diffattn_desc(n, lq, lk, hq, hk, d, _dtype_of(q, "q"), frame, scale or 0.0,
                                    q=_rows_of(q, row_q, "q"), k=_rows_of(k, row_k, "k"),

@@ -398,8 +398,17 @@ def _size(fn, desc) -> int:
     return out.value
 
 
+def _check_ints(values, names: str) -> None:
+    """ctypes would keep the low 32 bits of a number that its field does not hold."""
+    for v, name in zip(values, names.split()):
+        if not -1 << 31 <= v < 1 << 31:
+            raise ValueError("%s = %d does not fit 32 bits" % (name, v))
+
+
 def make_norm_desc(rows, c, dtype="bf16", eps=1e-5, x_pitch=0, y_pitch=0) -> NormDesc:
     """Fill an rt3d_norm_desc."""
+    if not 0 <= c < 1 << 31:
+        _check_ints((c,), "c")
     return NormDesc(rows, c, DTYPE_CODES[dtype], eps, x_pitch, y_pitch)
 
 
@@ -429,7 +438,10 @@ def make_rope_desc(n, grid, vecs, d, sections, dtype="bf16", base=10000.0, t0=0,
     """Fill an rt3d_rope_desc (``x``, ``y``: (pitch, batch) of their rows, tight
     where None)."""
     flags = (RT3D_ROPE_HALVES if halves else 0) | (RT3D_ROPE_INVERSE if inverse else 0)
-    return RopeDesc(n, *grid, vecs, d, *sections, t0, DTYPE_CODES[dtype], flags, base,
+    (t, h, w), (dt, dh, dw) = grid, sections
+    if not 0 <= n | t | h | w | vecs | d | dt | dh | dw | t0 < 1 << 31:  # (one test for all)
+        _check_ints((n, t, h, w, vecs, d, dt, dh, dw, t0), "n t h w vecs d dt dh dw t0")
+    return RopeDesc(n, t, h, w, vecs, d, dt, dh, dw, t0, DTYPE_CODES[dtype], flags, base,
                     x or _TIGHT, y or _TIGHT)
 
 
@@ -442,6 +454,10 @@ def make_diffattn_desc(n, lq, lk, hq, hk, d, dtype="bf16", frame=0, scale=0.0, q
                        k=None, v=None, d_o=None, dq=None, dk=None, dv=None) -> DiffAttnDesc:
     """Fill an rt3d_diffattn_desc; ``q`` to ``dv``: (pitch, batch) of a tensor's
     rows, tight where None."""
+    if not 0 <= n | lq | lk | hq | hk | d | frame < 1 << 31:
+        _check_ints((n, lq, lk, hq, hk, d, frame), "n lq lk hq hk d frame")
+    if scale and not ctypes.c_float(scale).value:
+        raise ValueError("scale is 0 in 32 bits, which asks for 1 / sqrt(d)")
     return DiffAttnDesc(n, lq, lk, hq, hk, d, DTYPE_CODES[dtype], frame, scale, q or _TIGHT,
                         o or _TIGHT, k or _TIGHT, v or _TIGHT, d_o or _TIGHT, dq or _TIGHT,
                         dk or _TIGHT, dv or _TIGHT)
