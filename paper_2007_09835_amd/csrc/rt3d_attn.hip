@@ -221,7 +221,7 @@ __global__ __launch_bounds__((Fwd<T, D, ROWS>::kThreads), (Fwd<T, D, ROWS>::kMin
         }
         float part[kMaps];
         bool over = probabilities(s, part);
-        if (__builtin_expect(!raised && __any(over), 0)) {
+        if (__builtin_expect(__any(over), 0)) {
 #pragma unroll
           for (int m = 0; m < kMaps; ++m) s[m] = f32x16{};
           scores(s, kt, j);

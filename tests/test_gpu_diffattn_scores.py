@@ -151,3 +151,30 @@ def test_scores_that_rise_along_the_keys(d, dtype, lq, lk):
         t[1].copy_(t[0].double())
     none = torch.zeros(lk, dtype=torch.bool)
     _forward_check(q, k, v, lam, (none, none), dtype, scale=1.0, far=512.0)
+
+
+@pytest.mark.parametrize("d,dtype", [(32, "bf16"), (64, "bf16"), (128, "bf16"), (64, "f32"), (96, "f32")])
+@pytest.mark.parametrize("lq,lk", [(33, 500), (70, 200), (30, 2100)])
+def test_rows_that_wait_for_a_score_beside_rows_that_rise(d, dtype, lq, lk):
+    """Every other row has scores of -inf for 150 keys; the scores of those between
+    rise by 160 nats over them, far past the range of a probability."""
+    q, k, v, _, lam = _inputs(8, 1, lq, lk, 1, 1, d, dtype)
+    late = torch.arange(lk) < 150
+    ramp = torch.linspace(0, 20, 150)
+    for qq, kk in zip(q, k):
+        qq[..., :2] = 0.0
+        kk[..., :2] = 0.0
+        qq[:, ::2, ..., 0] = 2.0 ** 84
+        kk[:, late, ..., 0] = -2.0 ** 84
+        qq[:, 1::2, ..., 1] = 8.0
+        kk[:, late, ..., 1] = ramp.to(k[0].dtype).to(kk.dtype).view(1, 150, 1, 1)
+    o = layers.diff_attention(q[0].cuda(), k[0].cuda(), v[0].cuda(), lam.cuda(), scale=1.0)
+    h = 0.0 if dtype == "f32" else refs.HALF[dtype]
+    more = dict(scale=1.0, h=h, tiny=refs.TINY[dtype])
+    half, tiny = refs.U if dtype == "f32" else 0.0, refs.TINY[dtype] * 4 + 1e-30
+    for rows, keys in ((slice(0, None, 2), ~late), (slice(1, None, 2), late | ~late)):
+        qq, kk = q[1][:, rows].contiguous(), k[1][:, keys].clone()
+        kk[..., 0] = 0.0
+        qq[..., 0] = 0.0
+        ref = refs.diff_attention(qq, kk, v[1][:, keys], lam.double(), **more)
+        refs.within(o[:, rows], ref["o"], ref["o_err"] + half * ref["o"].abs() + tiny, "o")
