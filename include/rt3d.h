@@ -524,6 +524,8 @@ rt3d_status rt3d_diffattn_bwd_workspace_size(const rt3d_diffattn_desc *desc, uin
  * heads that share a key head add up before the one rounding) and dlambda
  * (float32 [hq]).  Each may be NULL (not computed).  They are written, not added
  * to; rows behind q_len and k_len are zero.  d_o is not read behind q_len.
+ * Keys whose scores are -inf get zeros and change no other gradient, but that a key
+ * channel of -inf makes the same channel of dq NaN (0 times -inf).
  * Outputs must not overlap the inputs or each other.  Needs workspace of
  * rt3d_diffattn_bwd_workspace_size bytes (RT3D_ERR_BUFFER_TOO_SMALL otherwise). */
 rt3d_status rt3d_diffattn_bwd(const rt3d_diffattn_desc *desc, const void *q, const void *k,

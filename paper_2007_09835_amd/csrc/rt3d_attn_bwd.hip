@@ -223,14 +223,14 @@ __global__ __launch_bounds__(64 * WAVES, (Dq<T, D, WAVES>::kMinWaves)) void attn
     }
   }
   if (row >= rows) return;
-  dl = half_sum(dl);
+  dl = half_sum(in ? dl : 0.f);  // (rows behind the clip's end meet keys, which may be infinite)
   if (half == 0) {
     a.rowstat[(2 + split) * map + stat] = dl;
     if (begin == 0 && end <= 0) a.rowstat[stat] = a.rowstat[map + stat] = 0.f;
   }
   if (!a.dq) return;
-  // the softmax of a single key does not move
-  if (limit <= 1) {
+  // the softmax of a single key does not move, and rows behind the clip's end have none
+  if (!in || limit <= 1) {
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -444,8 +444,9 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       const unsigned qc = Q::at(across, tile_q), gc = Q::at(across, tile_g);
       unsigned kt = 0;
       if constexpr (F::kLdsK) kt = F::K::at(key_lane, keys);
-      // some pair of the tile is masked, or some row has a single key
-      const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
+      // some pair of the tile is masked (rows behind the clip's end are zeros, which an
+      // infinite key would turn into NaN), or some row has a single key
+      const bool masked = at + kRows > q_len || (a.frame && at < first_query(min(key_wave + 31, k_len - 1)));
       const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
       f32x16 dp = {}, pv;
       if constexpr (F::kAhead && DK) {
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (at + result_row(i, half) < from) s[i] = -INFINITY;
+            if (at + result_row(i, half) < from || at + result_row(i, half) >= q_len) s[i] = -INFINITY;
         }
         const float by = m ? -lam : 1.f;
 #pragma unroll

@@ -178,3 +178,29 @@ def test_rows_that_wait_for_a_score_beside_rows_that_rise(d, dtype, lq, lk):
         qq[..., 0] = 0.0
         ref = refs.diff_attention(qq, kk, v[1][:, keys], lam.double(), **more)
         refs.within(o[:, rows], ref["o"], ref["o_err"] + half * ref["o"].abs() + tiny, "o")
+
+
+@pytest.mark.parametrize("lq,lk,q_len", [(70, 200, None), (33, 900, None), (64, 200, [64, 40]), (128, 300, [1, 0])])
+@pytest.mark.parametrize("d,dtype", [(32, "bf16"), (64, "f16"), (128, "bf16"), (64, "f32"), (96, "f32")])
+def test_gradients_beside_hidden_keys(d, dtype, lq, lk, q_len):
+    """Keys hidden by a channel of -inf get no gradient and change nobody's, whatever
+    rows lie behind the clip's last query: only dq's own channel, 0 times -inf, is NaN."""
+    q, k, v, do, lam = _inputs(9, 2, lq, lk, 2, 1, d, dtype)
+    hidden = torch.arange(lk) // 8 % 3 == 1
+    _hide(q, k, (hidden, hidden), False)
+    args = [t[0].cuda() for t in (q, k, v)] + [lam.cuda()]
+    more = dict(q_len=None if q_len is None else torch.tensor(q_len, dtype=torch.int32).cuda())
+    _, saved = layers.diff_attention(*args, save=True, **more)
+    grads = layers.diff_attention_backward(do[0].cuda(), *args, saved, **more)
+    h = 0.0 if dtype == "f32" else refs.HALF[dtype]
+    ref = refs.diff_attention(q[1], k[1][:, ~hidden], v[1][:, ~hidden], lam.double(), 0, q_len, do=do[1], h=h,
+                              tiny=refs.TINY[dtype])
+    half, tiny = refs.U if dtype == "f32" else 0.0, refs.TINY[dtype] * 4 + 1e-30
+    for name, got in zip(("dq", "dk", "dv", "dlam"), grads):
+        want, err = ref[name], ref[name + "_err"]
+        if name in ("dk", "dv"):
+            assert not got[:, hidden].any(), name
+            got = got[:, ~hidden]
+        if name == "dq":
+            got, want, err = got[..., 1:], want[..., 1:], err[..., 1:]
+        refs.within(got, want, err + half * want.abs() + tiny, name)
