@@ -444,9 +444,8 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
       const unsigned qc = Q::at(across, tile_q), gc = Q::at(across, tile_g);
       unsigned kt = 0;
       if constexpr (F::kLdsK) kt = F::K::at(key_lane, keys);
-      // some pair of the tile is masked (rows behind the clip's end are zeros, which an
-      // infinite key would turn into NaN), or some row has a single key
-      const bool masked = at + kRows > q_len || (a.frame && at < first_query(min(key_wave + 31, k_len - 1)));
+      // some pair of the tile is masked, or some row has a single key
+      const bool masked = a.frame && at < first_query(min(key_wave + 31, k_len - 1));
       const bool lone = key_wave == 0 && (single_all || (single >= at && single < at + kRows));
       f32x16 dp = {}, pv;
       if constexpr (F::kAhead && DK) {
@@ -491,7 +490,13 @@ __global__ __launch_bounds__(64 * WAVES, (Dkv<T, D, WAVES>::kMinWaves)) void att
         if (masked) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (at + result_row(i, half) < from || at + result_row(i, half) >= q_len) s[i] = -INFINITY;
+            if (at + result_row(i, half) < from) s[i] = -INFINITY;
+        }
+        // rows behind the clip's end are zeros, which an infinite key would turn into NaN
+        if (__builtin_expect(at + kRows > q_len, 0)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (at + result_row(i, half) >= q_len) s[i] = -INFINITY;
         }
         const float by = m ? -lam : 1.f;
 #pragma unroll
