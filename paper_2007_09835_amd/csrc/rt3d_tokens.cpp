@@ -166,7 +166,9 @@ AttnArgs attn_args(const rt3d_diffattn_desc *d, const Shape &s, bool lengths) {
   AttnArgs a{};
   // Clips of unlike lengths would leave XCDs idle while others work: 8 x 6272
   // tokens, 8 heads, d 64, forward 1623 us with a clip's head on one XCD, 937 over
-  // all; 4 to 64 clips with 2 to 8 key heads 1.02-1.7x. Equal clips keep the shared L2.
+  // all; 4 to 64 clips with 2 to 8 key heads 1.02-1.7x. The lengths are on the device,
+  // so a call that is given any counts as unlike: clips that are in truth equal keep
+  // the shared L2 only where no lengths are given.
   a.spread = lengths ? 1 : 0;
   if (d->frame) a.sets = lengths ? 1 : static_cast<int32_t>(std::gcd<int64_t>(static_cast<int64_t>(d->n) * d->hk, 8));
   a.n = d->n;
