@@ -102,7 +102,8 @@ def maxpool3d(x: torch.Tensor, k, stride, dtype: str, out: Optional[torch.Tensor
 #
 # Inputs are tensors whose last dimension is dense; views into wider rows (a
 # projection's queries beside its keys, the filled part of a cache) are taken as
-# they are.  Results are new tensors unless ``out`` is given.  A call runs on the
+# they are.  Results are new tensors unless ``out`` is given, which may be x itself in
+# layer_norm and rope3d and must not overlap an input otherwise.  A call runs on the
 # device of its tensors, on ``stream`` (a torch stream of that device) or else on
 # that device's current stream; its results and workspace belong to that stream.
 # Gradients come from the backward calls; results carry no autograd graph, so with
