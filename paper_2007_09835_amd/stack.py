@@ -340,6 +340,7 @@ class TokenBlock:
         """(name, fn) of every launch of a pass over ``x`` (default: the input buffer)."""
         x = self.x if x is None else x
         heads = lambda b: b.view(self.batch, self.tokens, self.heads, 2 * self.d)
+        layers._no_graph(x)
         gather, own = [], [self.normed, self.row, self.o, self.mixed, self.y]
         if not x.is_contiguous():
             own.append(self.x)

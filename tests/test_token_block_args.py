@@ -27,3 +27,13 @@ def test_inputs_that_the_pass_would_overwrite():
     assert names == [name for name, _ in b.stages(b.x)] == [name for name, _ in b.stages(b.y.clone())]
     wide = torch.zeros(2, 2, 3, 3, 40, dtype=b.x.dtype)
     assert [name for name, _ in b.stages(wide[..., 8:])] == ["input"] + names
+
+
+def test_inputs_that_require_a_gradient():
+    """A gathered input must not carry its graph into the block's buffer."""
+    b = stack.TokenBlock(32, (2, 3, 3), 2, batch=2, device="cpu")
+    wide = torch.zeros(2, 2, 3, 3, 40, dtype=b.x.dtype, requires_grad=True)
+    for x in (wide[..., 8:], wide[..., 8:].contiguous()):
+        with pytest.raises(ValueError, match="no_grad"):
+            b.forward(x)
+        assert not b.x.requires_grad
