@@ -124,7 +124,7 @@ __device__ __forceinline__ float mean_of(float sum, float inv) {
 // steps off: much, where the row's spread is small (a constant row of 1000 in 32 bits:
 // y = -0.02 with it).  off, the distances' own mean, is what it lacks.
 __device__ __forceinline__ float variance(const float (&s)[2], float inv, float off) {
-  const float v = s[1] * inv - off * off;
+  const float v = fmaf(-off, off, s[1] * inv);  // (infinite, not NaN, where the squares are)
   return v < 0.f ? 0.f : v;
 }
 

@@ -52,3 +52,19 @@ def test_rows_of_small_spread(c, dtype):
     err = moved * rstd + (h.abs() + moved * rstd) * (spread + 8 * refs.U)
     half = refs.HALF[dtype]
     refs.within(y, ref, err + half * (ref.abs() + err) + refs.TINY[dtype], "y")
+
+
+@pytest.mark.parametrize("c", [7, 480, 921, 9000])
+@pytest.mark.parametrize("size", [1e18, 1e24, 1e30])
+def test_rows_whose_squares_pass_the_range(c, size):
+    """Where the sum of squares, about c size^2, passes 3.4e38, rstd is 0 and y is beta,
+    as the definition in 32 bits gives it; below that, y is as exact as ever."""
+    gen = torch.Generator().manual_seed(c)
+    x, beta = torch.randn(5, c, generator=gen) * size, torch.randn(c, generator=gen)
+    y = layers.layer_norm(x.cuda(), None, beta.cuda(), eps=EPS)
+    if c * size ** 2 > 4e38:
+        assert torch.equal(y.cpu(), beta.expand(5, c))
+        return
+    ref, h, mean, rstd = refs.layer_norm(x.double(), torch.ones(c).double(), beta.double(), EPS)
+    he = refs.norm_h_error(x.double(), h, rstd, c)
+    refs.within(y, ref, he + 4 * refs.U * (h.abs() + beta.double().abs()), "y")
